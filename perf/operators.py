@@ -130,7 +130,7 @@ def _mx4(seed, e, n, k):
     v = torch.ldexp(w, -s.unsqueeze(-1))
     a = v.abs()
     code = ((a > 0.25).byte() + (a > 0.75) + (a > 1.25) + (a > 1.75) + (a > 2.5) + (a > 3.5) + (a > 5))
-    return code + 8 * (v < 0), (s + 127).byte()
+    return code + 8 * (v < 0).byte(), (s + 127).byte()
 
 
 def _table(seed, e, n, k, fmt):
