@@ -56,6 +56,19 @@
  *             2*(j%16), 2*(j%16)+1 of word L0 + (n*W + j/16)*4; other bits 0;
  *   codebook  offset B0 = L0 + n*W*4 rounded up to a multiple of 16: entry e
  *             of sub-codebook t at B0 + (16*t + e)*2; total B0 + 128 bytes.
+ *
+ * MX4 (microscaled 4-bit floating point: the MXFP4 format of the OCP
+ * Microscaling specification, v1.0): blocks of 32 consecutive elements of a
+ * row with E2M1 codes q (bit 3 the sign, bits 0-2 the magnitudes 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6) and one E8M0 scale byte e, worth 2^(e - 127), or NaN for
+ * 255; W' = fp16_RNE(value(q) * 2^(e - 127)), which is exact for every blob
+ * that qx_quantize_mx4 writes; 4.25 bits per weight. Blob (b = 4, g = 32):
+ *   codes     offset 0: code i of a row in bits 4*(i%2).. of its byte i/2,
+ *             rows of k/2 bytes one after the other, n*k/2 bytes;
+ *   scales    offset n*k/2: byte n*(k/32) + j of (row n, block j).
+ * Both orders are plain row-major, so a row of activations and a row of
+ * weights look the same, and so do tensors of published checkpoints that hold
+ * the even code in the low bits.
  */
 #ifndef QX_H_
 #define QX_H_
@@ -70,7 +83,7 @@ extern "C" {
 /* HIP's stream handle (the same declaration as hip_runtime_api.h). */
 typedef struct ihipStream_t* hipStream_t;
 
-enum { QX_UNIFORM = 0, QX_CODEBOOK = 1, QX_Q4X = 2 };  /* qx_desc.kind */
+enum { QX_UNIFORM = 0, QX_CODEBOOK = 1, QX_Q4X = 2, QX_MX4 = 3 };  /* qx_desc.kind */
 enum { QX_OUT_F16 = 0, QX_OUT_CODES = 1 };   /* qx_dequant out_kind */
 
 enum {
@@ -85,10 +98,10 @@ enum {
  * Descriptor of one quantized matrix.
  *   n     rows (output features), n >= 0
  *   k     reduction length, a positive multiple of 128 (at most 1 << 20)
- *   bits  code width b: 3 or 4 (4 for QX_Q4X)
- *   group g: 32, 64 or 128 (64 for QX_Q4X)
- *   kind  QX_UNIFORM, QX_CODEBOOK or QX_Q4X; a QX_Q4X descriptor with other
- *         bits or group is malformed (QX_E_ARG)
+ *   bits  code width b: 3 or 4 (4 for QX_Q4X and QX_MX4)
+ *   group g: 32, 64 or 128 (64 for QX_Q4X, 32 for QX_MX4)
+ *   kind  QX_UNIFORM, QX_CODEBOOK, QX_Q4X or QX_MX4; a QX_Q4X or QX_MX4
+ *         descriptor with other bits or group is malformed (QX_E_ARG)
  *   flags must be 0
  */
 typedef struct {
@@ -111,7 +124,8 @@ typedef struct {
  * All pointers are host pointers. Pure and synchronous; returns QX_E_ARG for
  * a bad descriptor, a missing table, an out-of-range code or zero-point or a
  * non-finite scale, and QX_E_SIZE when cap < *packed_size (nothing written).
- * QX_Q4X descriptors are packed by qx_pack_q4x (QX_E_ARG here).
+ * QX_Q4X and QX_MX4 descriptors are packed by qx_pack_q4x and qx_pack_mx4
+ * (QX_E_ARG here).
  */
 int qx_pack_layout(const qx_desc* d, const uint8_t* codes, const uint16_t* scales,
                    const uint16_t* zeros, const uint16_t* codebook, void* packed, size_t cap,
@@ -137,12 +151,39 @@ int qx_pack_q4x(const qx_desc* d, const uint8_t* codes, const uint16_t* scales,
                 size_t* packed_size);
 
 /*
+ * qx_pack_mx4 -- write the packed blob of one MX4 matrix (host).
+ *   d          descriptor with kind QX_MX4, bits 4, group 32.
+ *   codes      uint8 [n][k] row-major, each < 16.
+ *   scales     uint8 [n][k/32], E8M0; any values.
+ *   packed, cap, packed_size as for qx_pack_layout.
+ * All pointers are host pointers. Pure and synchronous; returns QX_E_ARG for a
+ * descriptor of another kind, a missing input or an out-of-range code, and
+ * QX_E_SIZE when cap < *packed_size (nothing written).
+ */
+int qx_pack_mx4(const qx_desc* d, const uint8_t* codes, const uint8_t* scales, void* packed, size_t cap,
+                size_t* packed_size);
+
+/*
+ * qx_quantize_mx4 -- round fp16 rows to MX4 (device; weights or activations).
+ *   X fp16 [m][k] row-major, 16-byte aligned; k a positive multiple of 128 (at
+ *   most 1 << 20), m >= 0.
+ *   packed: the blob of a QX_MX4 descriptor of n = m rows (written, 16-byte
+ *   aligned), per block of 32: e = floor(log2 max|x|) - 2 + 127, and each x to
+ *   the nearest value(q) * 2^(e - 127), ties to the even code, larger ones to
+ *   +-6; signs are kept, zeros' too. A block of zeros gets e = 0. A block that
+ *   holds an infinity or a NaN gets e = 255 (every element NaN; its codes have
+ *   no meaning).
+ * Bit-exact with this definition. X and packed must not overlap.
+ */
+int qx_quantize_mx4(int32_t m, int32_t k, const uint16_t* X, void* packed, hipStream_t stream);
+
+/*
  * qx_dequant -- expand a packed blob into fp16 weights or raw codes (device).
  * Passage: the custom dequantization kernels of Section 2.4.
  *   packed   device blob written by qx_pack_layout (copied to the GPU).
  *   out_kind QX_OUT_F16: out = fp16 W' [n][k], uniform W' = fp16_RNE(s*(q-z))
  *            (the exact product, rounded once), codebook W' = C[q], Q4X
- *            W' = fp16_RNE(s*CB[t][q]).
+ *            W' = fp16_RNE(s*CB[t][q]), MX4 W' = fp16_RNE(value(q)*2^(e-127)).
  *            QX_OUT_CODES: out = uint8 codes [n][k].
  *   out      device buffer of n*k*2 (F16) or n*k (CODES) bytes.
  * Results are bit-exact with the definitions above.
@@ -165,7 +206,8 @@ int qx_gemv(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y
             hipStream_t stream);
 
 /*
- * qx_gemv_a8 -- y = W' x with x quantized to 8 bits (device; every kind).
+ * qx_gemv_a8 -- y = W' x with x quantized to 8 bits (device; every kind but
+ * QX_MX4, which gives QX_E_UNSUPPORTED).
  * Passage: activations are quantized to 8 bits and not below (Section 2.4);
  * the W3A8 configurations of Table 1 and Table 2's runs use 8-bit
  * round-to-nearest per-token activations.
@@ -203,7 +245,8 @@ int qx_quantize_a8(int32_t m, int32_t k, const uint16_t* X, int8_t* Xq, float* s
                    hipStream_t stream);
 
 /*
- * qx_gemm_a8 -- Y = X W'^T with 8-bit activations (device; every kind).
+ * qx_gemm_a8 -- Y = X W'^T with 8-bit activations (device; every kind but
+ * QX_MX4, which gives QX_E_UNSUPPORTED).
  * Passage: as qx_gemv_a8, for m activation rows (prefill of a W3A8 model; Table 2
  * runs Q4X prefill with 8-bit activations).
  *   Xq, sx as qx_quantize_a8 wrote them for the same k; Y fp16 [m][n]
@@ -233,10 +276,52 @@ int qx_gemm_a8(const qx_desc* d, const void* packed, int32_t m, const int8_t* Xq
  *   rows, m <= 48 by shape and format, each lane decoding its own chunks as in
  *   the GEMV), or, for m <= 4 where that measured faster, GEMV-style with every
  *   code decoded once for all rows. m = 0 or n = 0 is a no-op; m must be
- *   <= 65536. All formats, Q4X included. Deterministic.
+ *   <= 65536. All formats, Q4X and MX4 included. Deterministic.
  */
 int qx_gemm(const qx_desc* d, const void* packed, int32_t m, const uint16_t* X, uint16_t* Y,
             hipStream_t stream);
+
+/*
+ * qx_gemm_a4 -- Y = X' W'^T with both sides in MX4 (device).
+ *   d       a QX_MX4 descriptor (other kinds: QX_E_UNSUPPORTED); packed its blob.
+ *   Xq      device blob of m rows of the same k, as qx_quantize_mx4 writes it
+ *           (16-byte aligned); one Xq can feed every product that reads its rows.
+ *   Y       fp16 [m][n] row-major (written; 2-byte alignment suffices), rounded
+ *           to nearest-even from fp32 sums of exact products
+ *           value * value * 2^(e_w - 127) * 2^(e_x - 127) (scales are not
+ *           rounded to fp16 here; a scale of 255 on either side gives NaN).
+ * m = 0 or n = 0 is a no-op; m must be <= 65536. Deterministic.
+ */
+int qx_gemm_a4(const qx_desc* d, const void* packed, int32_t m, const void* Xq, uint16_t* Y, hipStream_t stream);
+
+/*
+ * qx_gemm_grouped -- rows of X times the matrix of their expert (device; every kind).
+ *   d        descriptor of each expert's matrix.
+ *   packed   the experts' blobs, that of expert e at byte e * stride; stride a
+ *            multiple of 16, at least the blob's size. 0 <= experts <= 1024.
+ *   offsets  device, int32 [experts + 1], not decreasing: rows offsets[e] ..
+ *            offsets[e+1] - 1 of X belong to expert e. It is read when the
+ *            work runs, so a router's output needs no copy to the host.
+ *   X, Y     fp16 [m][k] and [m][n] as for qx_gemm. Rows outside of
+ *            [offsets[0], offsets[experts]) are neither read nor written. Offsets
+ *            are held to [0, m] and an expert that ends before it begins has no
+ *            rows; which rows are written for offsets that decrease is not
+ *            specified, but never any outside of Y.
+ * Products, sums and rounding as qx_gemm's on the matrix cores. m = 0, n = 0 or
+ * no experts is a no-op; m must be <= 65536. QX_E_UNSUPPORTED when the tiles of
+ * m rows by n columns are more than one launch takes (4194304 blocks).
+ * Deterministic.
+ */
+int qx_gemm_grouped(const qx_desc* d, const void* packed, size_t stride, int32_t experts, int32_t m,
+                    const uint16_t* X, const int32_t* offsets, uint16_t* Y, hipStream_t stream);
+
+/*
+ * qx_gemm_a4_grouped -- qx_gemm_grouped with both sides in MX4 (device).
+ *   d, packed, stride, experts, offsets, Y as for qx_gemm_grouped; Xq the MX4
+ *   blob of all m rows, and the arithmetic, as for qx_gemm_a4.
+ */
+int qx_gemm_a4_grouped(const qx_desc* d, const void* packed, size_t stride, int32_t experts, int32_t m,
+                       const void* Xq, const int32_t* offsets, uint16_t* Y, hipStream_t stream);
 
 /* Static string for a status code ("unknown status" for values not listed). */
 const char* qx_status_str(int status);

@@ -28,7 +28,8 @@ in exact integer arithmetic.
 
 Modules: ``layout`` (pack/unpack of the packed layout), ``dequant``,
 ``matmul`` (fp64 products and the error metric), ``formats`` (sizes and
-bits-per-weight), ``q4x``, ``a8``.
+bits-per-weight), ``q4x``, ``a8``, ``mx4`` (the microscaled 4-bit format, and
+products grouped by expert).
 """
 from .layout import chunk_bit_positions, pack, unpack  # noqa: F401
 from .dequant import dequant, dequant_packed  # noqa: F401
@@ -36,3 +37,4 @@ from .matmul import gemv, gemm, normwise_rel_err  # noqa: F401
 from .formats import packed_size, bits_per_weight  # noqa: F401
 from . import q4x  # noqa: F401
 from . import a8  # noqa: F401
+from . import mx4  # noqa: F401

@@ -15,11 +15,18 @@ Functions keep the C names:
   qx_gemm(desc, packed, m, X, Y, stream=None)
   qx_quantize_a8(m, k, X, Xq, sx, stream=None)
   qx_gemm_a8(desc, packed, m, Xq, sx, Y, stream=None)
+  qx_pack_mx4(desc, codes, scales) -> uint8 numpy blob
+  qx_quantize_mx4(m, k, X, packed, stream=None)
+  qx_gemm_a4(desc, packed, m, Xq, Y, stream=None)
+  qx_gemm_grouped(desc, packed, m, X, offsets, Y, stream=None)
+  qx_gemm_a4_grouped(desc, packed, m, Xq, offsets, Y, stream=None)
   qx_status_str(status)
 Tensor arguments are torch CUDA tensors (HIP device memory); ``stream`` is a
 torch stream (default: the current stream). Before a device call the binding
 checks each tensor against the descriptor (device, dtype, contiguity, element
 count) and raises ValueError without launching anything when one does not fit.
+The calls of the microscaled and grouped products also check that every tensor
+lies on the current device, where they launch.
 """
 from __future__ import annotations
 
@@ -32,7 +39,7 @@ import numpy as np
 
 from . import _build
 
-QX_UNIFORM, QX_CODEBOOK, QX_Q4X = 0, 1, 2
+QX_UNIFORM, QX_CODEBOOK, QX_Q4X, QX_MX4 = 0, 1, 2, 3
 QX_OUT_F16, QX_OUT_CODES = 0, 1
 QX_OK, QX_E_ARG, QX_E_UNSUPPORTED, QX_E_SIZE, QX_E_HIP = 0, -1, -2, -3, -4
 
@@ -97,6 +104,14 @@ def load():
         L.qx_quantize_a8.restype = ctypes.c_int
         L.qx_gemm_a8.argtypes = [D, P, ctypes.c_int32, P, P, P, P]
         L.qx_gemm_a8.restype = ctypes.c_int
+        i32 = ctypes.c_int32
+        L.qx_pack_mx4.argtypes = [D, P, P, P, sz, ctypes.POINTER(sz)]
+        L.qx_quantize_mx4.argtypes = [i32, i32, P, P, P]
+        L.qx_gemm_a4.argtypes = [D, P, i32, P, P, P]
+        L.qx_gemm_grouped.argtypes = [D, P, sz, i32, i32, P, P, P, P]
+        L.qx_gemm_a4_grouped.argtypes = [D, P, sz, i32, i32, P, P, P, P]
+        for f in (L.qx_pack_mx4, L.qx_quantize_mx4, L.qx_gemm_a4, L.qx_gemm_grouped, L.qx_gemm_a4_grouped):
+            f.restype = ctypes.c_int
         L.qx_status_str.argtypes = [ctypes.c_int]
         L.qx_status_str.restype = ctypes.c_char_p
         _lib = L
@@ -159,6 +174,22 @@ def qx_pack_q4x(d: QxDesc, codes: np.ndarray, scales, selectors, codebook,
     return out[:size.value]
 
 
+def qx_pack_mx4(d: QxDesc, codes: np.ndarray, scales, out: Optional[np.ndarray] = None) -> np.ndarray:
+    """MX4 blob (host uint8 array): E2M1 codes [n][k] (< 16), E8M0 scales [n][k/32]."""
+    codes = np.ascontiguousarray(codes, dtype=np.uint8)
+    scales = np.ascontiguousarray(scales, dtype=np.uint8)
+    size = ctypes.c_size_t(0)
+    L = load()
+    _check(L.qx_pack_mx4(ctypes.byref(d), None, None, None, 0, ctypes.byref(size)), "qx_pack_mx4")
+    if codes.size != d.n * d.k or scales.size != d.n * d.k // 32:
+        raise ValueError(f"codes {codes.shape} and scales {scales.shape} do not fit {d}")
+    if out is None:
+        out = np.empty(size.value, np.uint8)
+    _check(L.qx_pack_mx4(ctypes.byref(d), _np_ptr(codes), _np_ptr(scales), _np_ptr(out), out.nbytes,
+                         ctypes.byref(size)), "qx_pack_mx4")
+    return out[:size.value]
+
+
 def _chk(t, name: str, dtype, numel: int):
     """Check that `t` is a contiguous device tensor of `dtype` (None: any) holding at least
     `numel` elements (the kernels read and write exactly the sizes the descriptor implies)."""
@@ -186,8 +217,11 @@ def _ptrs(*tensors):
 def _blob_size(n: int, k: int, bits: int, group: int, kind: int, flags: int) -> int:
     size = ctypes.c_size_t(0)
     L = load()
-    fn = L.qx_pack_q4x if kind == QX_Q4X else L.qx_pack_layout
     d = QxDesc(n, k, bits, group, kind, flags)
+    if kind == QX_MX4:
+        _check(L.qx_pack_mx4(ctypes.byref(d), None, None, None, 0, ctypes.byref(size)), "packed size")
+        return size.value
+    fn = L.qx_pack_q4x if kind == QX_Q4X else L.qx_pack_layout
     _check(fn(ctypes.byref(d), None, None, None, None, None, 0, ctypes.byref(size)), "packed size")
     return size.value
 
@@ -273,6 +307,90 @@ def qx_gemm_a8(d: QxDesc, packed, m: int, Xq, sx, Y, stream=None) -> None:
     _check(load().qx_gemm_a8(ctypes.byref(d), p, m, xq, s_, y, _stream(stream)), "qx_gemm_a8")
 
 
+def _here(stream, *tensors):
+    """The raw stream, once every tensor is known to lie on the current device (a launch goes to
+    the current device, whatever the tensors' own)."""
+    import torch
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t.device.index != at:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{at}")
+    if stream is not None and stream.device.index != at:
+        raise ValueError(f"stream of {stream.device}, but the current device is cuda:{at}")
+    return _stream(stream)
+
+
+def qx_quantize_mx4(m: int, k: int, X, packed, stream=None) -> None:
+    import torch
+    m, k = int(m), int(k)
+    _rows(X, m, k, "X")
+    _chk(X, "X", torch.float16, m * k)
+    _chk(packed, "packed", torch.uint8, m * k // 32 * 17)
+    s = _here(stream, X, packed)
+    _check(load().qx_quantize_mx4(m, k, *_ptrs(X, packed), s), "qx_quantize_mx4")
+
+
+def _mx4_rows(Xq, m: int, k: int):
+    import torch
+    _chk(Xq, "Xq", torch.uint8, m * k // 32 * 17)
+
+
+def qx_gemm_a4(d: QxDesc, packed, m: int, Xq, Y, stream=None) -> None:
+    import torch
+    m = int(m)
+    _chk_packed(d, packed)
+    _mx4_rows(Xq, m, d.k)
+    _chk(Y, "Y", torch.float16, m * d.n)
+    s = _here(stream, packed, Xq, Y)
+    p, x, y = _ptrs(packed, Xq, Y)
+    _check(load().qx_gemm_a4(ctypes.byref(d), p, m, x, y, s), "qx_gemm_a4")
+
+
+def _chk_experts(d: QxDesc, packed, offsets):
+    """(experts, bytes between their blobs) of a uint8 tensor [experts][at least the blob's size]."""
+    import torch
+    _chk(packed, "packed", torch.uint8, 0)
+    if packed.dim() != 2 or packed.shape[1] % 16 or packed.shape[1] < qx_blob_size(d):
+        raise ValueError(f"packed: shape {tuple(packed.shape)}, expected [experts][bytes], bytes a multiple of 16 "
+                         f"and at least {qx_blob_size(d)}")
+    _chk(offsets, "offsets", torch.int32, packed.shape[0] + 1)
+    if offsets.numel() != packed.shape[0] + 1:
+        raise ValueError(f"offsets: {offsets.numel()} elements, {packed.shape[0] + 1} expected")
+    return packed.shape
+
+
+def qx_gemm_grouped(d: QxDesc, packed, m: int, X, offsets, Y, stream=None) -> None:
+    import torch
+    m = int(m)
+    experts, stride = _chk_experts(d, packed, offsets)
+    _rows(X, m, d.k, "X")
+    _chk(X, "X", torch.float16, m * d.k)
+    _chk(Y, "Y", torch.float16, m * d.n)
+    s = _here(stream, packed, X, offsets, Y)
+    p, x, o, y = _ptrs(packed, X, offsets, Y)
+    _check(load().qx_gemm_grouped(ctypes.byref(d), p, stride, experts, m, x, o, y, s), "qx_gemm_grouped")
+
+
+def qx_gemm_a4_grouped(d: QxDesc, packed, m: int, Xq, offsets, Y, stream=None) -> None:
+    import torch
+    m = int(m)
+    experts, stride = _chk_experts(d, packed, offsets)
+    _mx4_rows(Xq, m, d.k)
+    _chk(Y, "Y", torch.float16, m * d.n)
+    s = _here(stream, packed, Xq, offsets, Y)
+    p, x, o, y = _ptrs(packed, Xq, offsets, Y)
+    _check(load().qx_gemm_a4_grouped(ctypes.byref(d), p, stride, experts, m, x, o, y, s), "qx_gemm_a4_grouped")
+
+
+def quantize_mx4(X, stream=None) -> "PackedWeight":
+    """An fp16 device tensor [m][k], weights or activations, rounded to MX4 where it lies."""
+    import torch
+    m, k = X.shape
+    out = torch.empty(m * k // 32 * 17, dtype=torch.uint8, device=X.device)
+    qx_quantize_mx4(m, k, X, out, stream)
+    return PackedWeight.from_blob(QxDesc(m, k, 4, 32, QX_MX4, 0), out)
+
+
 def quantize_a8(X, stream=None):
     """(Xq int8 [m][k], sx fp32 [m]) of an fp16 [m][k] device tensor."""
     import torch
@@ -296,11 +414,21 @@ class PackedWeight:
     @classmethod
     def from_quant(cls, q, device="cuda") -> "PackedWeight":
         """From an object with n, k, bits, group, kind, codes, scales, zeros, codebook
-        (and selectors for Q4X)."""
+        (and selectors for Q4X; MX4: codes and E8M0 scales)."""
         d = desc(q.n, q.k, q.bits, q.group, q.kind)
+        if q.kind == QX_MX4:
+            return cls(d, qx_pack_mx4(d, q.codes, q.scales), device)
         if q.kind == QX_Q4X:
             return cls(d, qx_pack_q4x(d, q.codes, q.scales, q.selectors, q.codebook), device)
         return cls(d, qx_pack_layout(d, q.codes, q.scales, q.zeros, q.codebook), device)
+
+    @classmethod
+    def from_blob(cls, d: QxDesc, data) -> "PackedWeight":
+        """Around a blob that is in device memory already (a uint8 tensor; not copied)."""
+        _chk_packed(d, data)
+        self = cls.__new__(cls)
+        self.desc, self.nbytes, self.data = d, qx_blob_size(d), data
+        return self
 
     def dequant(self, out_kind: int = QX_OUT_F16, stream=None):
         import torch
@@ -337,4 +465,59 @@ class PackedWeight:
         if Y is None:
             Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
         qx_gemm(self.desc, self.data, m, X, Y, stream)
+        return Y
+
+    def gemm_a4(self, Xq: "PackedWeight", Y=None, stream=None):
+        """Of the rows that quantize_mx4 wrote."""
+        import torch
+        m = _rows_of(Xq, self.desc.k)
+        if Y is None:
+            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
+        qx_gemm_a4(self.desc, self.data, m, Xq.data, Y, stream)
+        return Y
+
+
+def _rows_of(Xq: PackedWeight, k: int) -> int:
+    if Xq.desc.kind != QX_MX4 or Xq.desc.k != k:
+        raise ValueError(f"rows of {Xq.desc}, expected QX_MX4 rows of k = {k}")
+    return Xq.desc.n
+
+
+class PackedExperts:
+    """Packed matrices of one descriptor, resident in device memory, for products of rows that are
+    sorted by expert."""
+
+    def __init__(self, d: QxDesc, data):
+        """data: uint8 device tensor [experts][bytes], a blob at the head of every row; bytes a
+        multiple of 16 (not copied)."""
+        self.desc, self.data = d, data
+
+    @classmethod
+    def stack(cls, weights) -> "PackedExperts":
+        """From PackedWeights of one descriptor, copied side by side."""
+        import torch
+        d, size = weights[0].desc, weights[0].nbytes
+        if any(bytes(w.desc) != bytes(d) for w in weights):
+            raise ValueError("experts of different descriptors")
+        data = torch.zeros((len(weights), (size + 15) // 16 * 16), dtype=torch.uint8, device=weights[0].data.device)
+        for e, w in enumerate(weights):
+            data[e, :size] = w.data[:size]
+        return cls(d, data)
+
+    def gemm(self, X, offsets, Y=None, stream=None):
+        """Rows offsets[e] .. offsets[e+1] - 1 of X times expert e; offsets int32 on the device."""
+        import torch
+        m = X.shape[0]
+        if Y is None:
+            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
+        qx_gemm_grouped(self.desc, self.data, m, X, offsets, Y, stream)
+        return Y
+
+    def gemm_a4(self, Xq: PackedWeight, offsets, Y=None, stream=None):
+        """The same with MX4 weights and the rows that quantize_mx4 wrote."""
+        import torch
+        m = _rows_of(Xq, self.desc.k)
+        if Y is None:
+            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
+        qx_gemm_a4_grouped(self.desc, self.data, m, Xq.data, offsets, Y, stream)
         return Y

@@ -139,6 +139,7 @@ static int launch_dequant_t(const qx_desc* d, const void* packed, int out_kind, 
 }
 
 int launch_dequant(const qx_desc* d, const void* packed, int out_kind, void* out, hipStream_t s) {
+  if (d->kind == QX_MX4) return launch_dequant_mx4(d, packed, out_kind, out, s);
 #define QX_DQ_CASE(B, K, G) \
   if (d->bits == B && d->kind == K && d->group == G) return launch_dequant_t<B, K, G>(d, packed, out_kind, out, s);
   QX_DQ_CASE(3, 0, 32) QX_DQ_CASE(3, 0, 64) QX_DQ_CASE(3, 0, 128)

@@ -548,6 +548,7 @@ static int launch_gemm_t(const qx_desc* d, const void* packed, int m, const void
 
 int launch_gemm(const qx_desc* d, const void* packed, int m, const uint16_t* X, uint16_t* Y,
                 hipStream_t s) {
+  if (d->kind == QX_MX4) return launch_gemm_mx4(d, packed, m, X, Y, s);
 #define QX_GEMM_CASE(B, K, G) \
   if (d->bits == B && d->kind == K && d->group == G) return launch_gemm_t<B, K, G>(d, packed, m, X, nullptr, Y, s);
   QX_GEMM_CASE(3, 0, 32) QX_GEMM_CASE(3, 0, 64) QX_GEMM_CASE(3, 0, 128)

@@ -48,6 +48,7 @@
 // most 64 * 15 * 127), those of Q4X round as fp32 sums do.
 #include <type_traits>
 
+#include "expert_tiles.h"
 #include "gemm_tile_plan.h"
 #include "qx_device.h"
 
@@ -136,12 +137,12 @@ __device__ __forceinline__ h8_t tile_frag(const RawFrag<BITS, KIND>& gd, const D
   }
 }
 
-template <int BITS, int KIND, int G, int MT, int NT, int WM, int SC, int KS, bool A8,
+template <int BITS, int KIND, int G, int MT, int NT, int WM, int SC, int KS, bool A8, bool GROUPED,
           int THREADS = TileShape<BITS, KIND, G, MT, NT, WM, SC, KS>::kThreads,
           int WAVES = TileShape<BITS, KIND, G, MT, NT, WM, SC, KS>::kWaves>
 __global__ __launch_bounds__(THREADS, WAVES) void gemm_tile_kernel(
     const char* __restrict__ packed, const void* __restrict__ Xv, const float* __restrict__ sx,
-    uint16_t* __restrict__ Y, int n, int k, int m, int nx, int my, int groups) {
+    uint16_t* __restrict__ Y, int n, int k, int m, int nx, int my, int groups, Experts ex) {
   using TS = TileShape<BITS, KIND, G, MT, NT, WM, SC, KS>;
   using TR = TileReads<BITS, KIND, G, MT, NT, WM, SC, KS, A8>;
   constexpr int NTH = TR::NTH, BM = TS::BM, BN = TS::BN, NG = TS::NG, kXB = TR::kXB, kMRow = TR::kMRow;
@@ -156,11 +157,21 @@ __global__ __launch_bounds__(THREADS, WAVES) void gemm_tile_kernel(
   char* const mts = cts + 2 * TS::kCBuf;
   uint32_t* const q4lut = reinterpret_cast<uint32_t*>(lds + KS * TS::kWaveLds);
 
-  const int total = nx * my, share = (total + 7) >> 3, at = blockIdx.x >> 3;
-  const int tile = (int)(blockIdx.x & 7) * share + at;
-  if (tile >= total) return;  // whole block, before any barrier
-  const TileAt block = tile_at(tile, nx, my, groups);
-  const int n0 = block.bn * BN, m0 = block.bm * BM;
+  int n0, m0;
+  if constexpr (GROUPED) {  // the tile's rows of one expert, as if they were a product of their own
+    const ExpertTile own = expert_tile(ex, m, BM, nx, blockIdx.x);
+    if (own.rows == 0) return;  // whole block, before any barrier
+    packed += (size_t)own.expert * ex.stride;
+    Xv = static_cast<const char*>(Xv) + (size_t)own.row0 * k * kXB;
+    Y += (size_t)own.row0 * n;
+    n0 = own.nt * BN, m0 = 0, m = own.rows;
+  } else {
+    const int total = nx * my, share = (total + 7) >> 3, at = blockIdx.x >> 3;
+    const int tile = (int)(blockIdx.x & 7) * share + at;
+    if (tile >= total) return;  // whole block, before any barrier
+    const TileAt block = tile_at(tile, nx, my, groups);
+    n0 = block.bn * BN, m0 = block.bm * BM;
+  }
   const int C = k >> 7, G_row = k / G;
   const size_t meta_off = (size_t)n * k * BITS / 8;
   const int t = KS > 1 ? threadIdx.x & 63 : threadIdx.x, lane = t & 63, g = lane >> 4, li = lane & 15;
@@ -510,8 +521,8 @@ int launch_cfg(const qx_desc* d, const void* packed, int m, const void* X, const
   static_assert(TS::kLds <= kLdsBytes, "LDS");
   const int nx = (d->n + TS::BN - 1) / TS::BN, my = (m + TS::BM - 1) / TS::BM;
   const unsigned blocks = ((unsigned)nx * (unsigned)my + 7u) / 8u * 8u;
-  hipLaunchKernelGGL((gemm_tile_kernel<BITS, KIND, G, MT, NT, WM, SC, KS, A8>), dim3(blocks), dim3(TS::kThreads), 0,
-                     s, static_cast<const char*>(packed), X, sx, Y, d->n, d->k, m, nx, my, tile_groups(my));
+  hipLaunchKernelGGL((gemm_tile_kernel<BITS, KIND, G, MT, NT, WM, SC, KS, A8, false>), dim3(blocks), dim3(TS::kThreads), 0,
+                     s, static_cast<const char*>(packed), X, sx, Y, d->n, d->k, m, nx, my, tile_groups(my), Experts{});
   return hipGetLastError() == hipSuccess ? QX_OK : QX_E_HIP;
 }
 
@@ -540,6 +551,21 @@ int run(const qx_desc* d, const void* packed, int m, const void* X, const float*
   }
 }
 
+// Products grouped by expert, of fp16 rows: shape S.
+template <int BITS, int KIND, int G, int S>
+int launch_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X, uint16_t* Y,
+                   hipStream_t s) {
+  constexpr ShapeCost C = kShape[S];
+  using TS = TileShape<BITS, KIND, G, C.mt, C.nt, C.wm, C.sc, C.ks>;
+  static_assert(TS::kLds <= kLdsBytes, "LDS");
+  const int nx = (int)(((long)d->n + TS::BN - 1) / TS::BN);
+  const unsigned blocks = expert_blocks(ex, m, TS::BM, nx);
+  if (blocks == 0) return QX_E_UNSUPPORTED;
+  hipLaunchKernelGGL((gemm_tile_kernel<BITS, KIND, G, C.mt, C.nt, C.wm, C.sc, C.ks, false, true>), dim3(blocks),
+                     dim3(TS::kThreads), 0, s, static_cast<const char*>(packed), X, nullptr, Y, d->n, d->k, m, nx, 0, 0, ex);
+  return hipGetLastError() == hipSuccess ? QX_OK : QX_E_HIP;
+}
+
 }  // namespace
 
 bool gemm_tile_applies(const qx_desc* d, int m, bool a8) { return pick_shape(d, m, a8) != kShapes; }
@@ -553,6 +579,20 @@ int launch_gemm_tile(const qx_desc* d, const void* packed, int m, const void* X,
                          : run<B, K, G, false>(d, packed, m, X, sx, Y, shape, s);
   QX_TILE_FORMATS(QX_TILE_RUN)
 #undef QX_TILE_RUN
+  return QX_E_UNSUPPORTED;
+}
+
+int launch_gemm_tile_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X,
+                             uint16_t* Y, hipStream_t s) {
+  // rows of an expert, were they shared evenly: up to 32 the tiles with k split over a block's
+  // waves, whose blocks are many and short
+  const bool few = m <= 32 * ex.count;
+#define QX_TILE_GROUPED(B, K, G)                                                     \
+  if (d->bits == B && d->kind == K && d->group == G)                                 \
+    return few ? launch_grouped<B, K, G, kH>(d, packed, ex, m, X, Y, s)              \
+               : launch_grouped<B, K, G, kE>(d, packed, ex, m, X, Y, s);
+  QX_TILE_FORMATS(QX_TILE_GROUPED)
+#undef QX_TILE_GROUPED
   return QX_E_UNSUPPORTED;
 }
 

@@ -391,6 +391,7 @@ static int launch_gemv_t(const qx_desc* d, const void* packed, const uint16_t* x
 
 int launch_gemv(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y,
                 hipStream_t s) {
+  if (d->kind == QX_MX4) return launch_gemv_mx4(d, packed, x, y, s);
 #define QX_GEMV_CASE(B, K, G) \
   if (d->bits == B && d->kind == K && d->group == G) return launch_gemv_t<B, K, G>(d, packed, x, y, s);
   QX_GEMV_CASE(3, 0, 32) QX_GEMV_CASE(3, 0, 64) QX_GEMV_CASE(3, 0, 128)

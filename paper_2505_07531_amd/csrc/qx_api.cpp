@@ -5,36 +5,11 @@
 #include <thread>
 #include <vector>
 
-#include "qx_internal.h"
+#include "qx_check.h"
+
+using namespace qx;
 
 namespace {
-
-constexpr int kMaxK = 1 << 20;
-
-// Well-formed: the fields make sense. Supported: a kernel instance exists.
-int check_desc(const qx_desc* d) {
-  if (d == nullptr) return QX_E_ARG;
-  if (d->flags != 0 || d->n < 0 || d->k <= 0 || d->k % 128 != 0 || d->k > kMaxK) return QX_E_ARG;
-  if (d->kind != QX_UNIFORM && d->kind != QX_CODEBOOK && d->kind != QX_Q4X) return QX_E_ARG;
-  if (d->kind == QX_Q4X && (d->bits != 4 || d->group != 64)) return QX_E_ARG;  // fixed by the format
-  if (d->bits < 1 || d->bits > 8 || d->group <= 0 || d->k % d->group != 0) return QX_E_ARG;
-  if (d->bits != 3 && d->bits != 4) return QX_E_UNSUPPORTED;
-  if (d->group != 32 && d->group != 64 && d->group != 128) return QX_E_UNSUPPORTED;
-  return QX_OK;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned2(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 1u) == 0; }
-
-size_t meta_bytes_per_group(const qx_desc* d) {
-  return d->kind == QX_UNIFORM ? 4 : 2u * (1u << d->bits);
-}
-
-size_t packed_bytes(const qx_desc* d) {
-  if (d->kind == QX_Q4X) return qx::q4x_offsets(d->n, d->k).total;
-  const size_t n = (size_t)d->n, k = (size_t)d->k;
-  return n * k * d->bits / 8 + n * (k / d->group) * meta_bytes_per_group(d);
-}
 
 // binary16 helpers for validation only
 bool half_finite(uint16_t h) { return ((h >> 10) & 31) != 31; }
@@ -90,7 +65,7 @@ int qx_pack_layout(const qx_desc* d, const uint8_t* codes, const uint16_t* scale
                    size_t* packed_size) {
   const int st = check_desc(d);
   if (st != QX_OK) return st;
-  if (packed_size == nullptr || d->kind == QX_Q4X) return QX_E_ARG;
+  if (packed_size == nullptr || d->kind == QX_Q4X || d->kind == QX_MX4) return QX_E_ARG;
   const size_t total = packed_bytes(d);
   *packed_size = total;
   if (packed == nullptr) return QX_OK;
@@ -203,7 +178,7 @@ int qx_gemv_a8(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t
                hipStream_t stream) {
   const int st = check_desc(d);
   if (st != QX_OK) return st;
-  if (d->k > 88 * 128) return QX_E_UNSUPPORTED;
+  if (d->k > 88 * 128 || d->kind == QX_MX4) return QX_E_UNSUPPORTED;
   if (d->n == 0) return QX_OK;
   if (packed == nullptr || x == nullptr || y == nullptr) return QX_E_ARG;
   if (!aligned16(packed) || !aligned16(x) || !aligned2(y)) return QX_E_ARG;
@@ -211,7 +186,7 @@ int qx_gemv_a8(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t
 }
 
 int qx_quantize_a8(int32_t m, int32_t k, const uint16_t* X, int8_t* Xq, float* sx, hipStream_t stream) {
-  if (m < 0 || m > 65536 || k <= 0 || k % 128 != 0 || k > kMaxK) return QX_E_ARG;
+  if (m < 0 || m > kMaxRows || k <= 0 || k % 128 != 0 || k > kMaxK) return QX_E_ARG;
   if (m == 0) return QX_OK;
   if (X == nullptr || Xq == nullptr || sx == nullptr) return QX_E_ARG;
   if (!aligned16(X) || !aligned16(Xq) || (reinterpret_cast<uintptr_t>(sx) & 3u) != 0) return QX_E_ARG;
@@ -222,7 +197,8 @@ int qx_gemm_a8(const qx_desc* d, const void* packed, int32_t m, const int8_t* Xq
                uint16_t* Y, hipStream_t stream) {
   const int st = check_desc(d);
   if (st != QX_OK) return st;
-  if (m < 0 || m > 65536) return QX_E_ARG;
+  if (d->kind == QX_MX4) return QX_E_UNSUPPORTED;
+  if (m < 0 || m > kMaxRows) return QX_E_ARG;
   if (m == 0 || d->n == 0) return QX_OK;
   if (packed == nullptr || Xq == nullptr || sx == nullptr || Y == nullptr) return QX_E_ARG;
   if (!aligned16(packed) || !aligned16(Xq) || (reinterpret_cast<uintptr_t>(sx) & 3u) != 0 || !aligned2(Y))
@@ -243,10 +219,11 @@ int qx_gemm(const qx_desc* d, const void* packed, int32_t m, const uint16_t* X, 
             hipStream_t stream) {
   const int st = check_desc(d);
   if (st != QX_OK) return st;
-  if (m < 0 || m > 65536) return QX_E_ARG;
+  if (m < 0 || m > kMaxRows) return QX_E_ARG;
   if (m == 0 || d->n == 0) return QX_OK;
   if (packed == nullptr || X == nullptr || Y == nullptr) return QX_E_ARG;
   if (!aligned16(packed) || !aligned16(X) || !aligned2(Y)) return QX_E_ARG;
+  if (d->kind == QX_MX4) return qx::launch_gemm(d, packed, m, X, Y, stream);
   if (m == 1 && qx::gemv_multi_applies(d, 1)) return qx::launch_gemv(d, packed, X, Y, stream);
   if (!qx::gemm_skinny_applies(d, m) && qx::gemm_tile_applies(d, m, false))
     return qx::launch_gemm_tile(d, packed, m, X, nullptr, Y, stream);

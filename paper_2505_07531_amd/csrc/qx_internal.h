@@ -27,6 +27,14 @@ __host__ __device__ inline Q4xOffsets q4x_offsets(int n, int k) {
   return o;
 }
 
+// Experts of a grouped product: blobs `stride` bytes apart, and (device) the first row of each
+// and the end of the last. No experts: one matrix for all rows.
+struct Experts {
+  size_t stride;
+  int count;
+  const int32_t* offsets;
+};
+
 int launch_dequant(const qx_desc* d, const void* packed, int out_kind, void* out, hipStream_t s);
 int launch_gemv(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y,
                 hipStream_t s);
@@ -86,5 +94,19 @@ bool gemm_skinny_applies(const qx_desc* d, int m);
 
 int launch_gemm_skinny(const qx_desc* d, const void* packed, int m, const uint16_t* X, uint16_t* Y,
                        hipStream_t s);
+
+// Microscaled 4-bit weights (mx4_convert.hip, mx4_gemm.hip): rows of fp16 or of the same format.
+int launch_quantize_mx4(int m, int k, const uint16_t* X, void* packed, hipStream_t s);
+int launch_dequant_mx4(const qx_desc* d, const void* packed, int out_kind, void* out, hipStream_t s);
+int launch_gemv_mx4(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y, hipStream_t s);
+int launch_gemm_mx4(const qx_desc* d, const void* packed, int m, const uint16_t* X, uint16_t* Y, hipStream_t s);
+int launch_gemm_a4(const qx_desc* d, const void* packed, int m, const void* Xq, uint16_t* Y, hipStream_t s);
+int launch_gemm_mx4_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X,
+                            uint16_t* Y, hipStream_t s);
+int launch_gemm_a4_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const void* Xq,
+                           uint16_t* Y, hipStream_t s);
+// fp16 rows grouped by expert, the other kinds (gemm_tile.hip).
+int launch_gemm_tile_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X,
+                             uint16_t* Y, hipStream_t s);
 
 }  // namespace qx
