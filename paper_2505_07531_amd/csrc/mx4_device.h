@@ -25,7 +25,8 @@ __device__ __forceinline__ f4_t mfma_mx4(u32x4 a, uint32_t sa, u32x4 b, uint32_t
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 4, 4, 0, (int)sa, 0, (int)sb);
 }
 
-// Four neighbouring columns of a row of Y, which may start at any multiple of 2 bytes.
+// Neighbouring columns of a row of Y, which may start at any multiple of 2 bytes.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 __device__ __forceinline__ void store4(uint16_t* dst, f4_t v, int left) {  // left: columns to the row's end
   uint32_t h[4];

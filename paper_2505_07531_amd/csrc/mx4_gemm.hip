@@ -1,94 +1,93 @@
-// Products with microscaled 4-bit weights, Y[m][n] = sum_k X[m][k] W'[n][k], for fp16 rows X and for
-// rows of the same format, of one matrix or grouped by expert.
-//
-// A lane holds one block of 32 codes of a weight row (16 bytes) and the four lane groups of a wave
-// four neighbouring blocks, 128 of k. For fp16 rows the codes are converted with their scale, two a
-// v_cvt_scalef32_pk_f16_fp4, into the operands of four v_mfma_f32_16x16x32_f16; for rows of the same
-// format both sides go to v_mfma_scale_f32_16x16x128_f8f6f4 as they are. Weights are the first
-// operand, so that a lane ends with four neighbouring columns of Y.
-#include "mx4_device.h"
+// Products of fp16 rows with microscaled 4-bit weights: the launcher of the tiles (mx4_tile.h), and the
+// kernel for one row.
+#include "mx4_tile.h"
 
 namespace qx {
 namespace {
 
-// One wave: 16 weight rows, 16 * MT activation rows, all of k, operands straight from memory.
-template <bool A4, bool GROUPED, int MT>
-__global__ __launch_bounds__(256) void mx4_gemm_kernel(const char* __restrict__ packed, const char* __restrict__ X,
-                                                       uint16_t* __restrict__ Y, int n, int k, int m, int nx, Experts ex) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, li = lane & 15;
-  int n0 = (int)(blockIdx.x % nx) * 64 + wave * 16, m0 = (int)(blockIdx.x / nx) * 16 * MT, rows = min(m - m0, 16 * MT);
-  const char* W = packed;
-  if constexpr (GROUPED) {
-    const ExpertTile t = expert_tile(ex, m, 16 * MT, nx, blockIdx.x);
-    if (t.rows == 0) return;
-    n0 = t.nt * 64 + wave * 16, m0 = t.row0, rows = t.rows, W += (size_t)t.expert * ex.stride;
-  }
-  const int G = k >> 5;
-  const size_t wrow = (size_t)min(n0 + li, n - 1);
-  const char* wc = W + wrow * (k >> 1) + 16 * g;
-  const uint8_t* ws = reinterpret_cast<const uint8_t*>(W + (size_t)n * (k >> 1)) + wrow * G + g;
-  size_t xrow[MT];
+constexpr int kGemvRows = 4, kGemvWaves = 8;
+
+// One row. A lane takes one block of 32 codes of each of kGemvRows weight rows and holds the 32 values
+// of x that belong to it in registers; a wave takes 64 neighbouring blocks (2048 k), SEG waves a whole
+// row, or more in turns. Read-bound: 17 bytes of codes and scale for 32 products, 16 conversions and 16
+// v_dot2. No x in LDS and no barrier before the products: only the SEG sums of a row meet there.
+template <int SEG>
+__global__ __launch_bounds__(64 * kGemvWaves) void mx4_gemv_kernel(const char* __restrict__ packed,
+                                                                  const u32x4* __restrict__ x, uint16_t* __restrict__ y,
+                                                                  int n, int k) {
+  constexpr int kRows = kGemvRows * (kGemvWaves / SEG);  // of a block
+  __shared__ float sums[kRows][SEG];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int seg = wave % SEG, part = wave / SEG, G = k >> 5, row0 = blockIdx.x * kRows + part * kGemvRows;
+  const uint8_t* const scales = reinterpret_cast<const uint8_t*>(packed + (size_t)n * (k >> 1));
+  float sum[kGemvRows] = {};
+  for (int b0 = seg * 64; b0 < G; b0 += SEG * 64) {
+    const int b = min(b0 + lane, G - 1);
+    u32x4 xv[4], q[kGemvRows];
+    uint32_t s[kGemvRows];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) xrow[t] = (size_t)m0 + min(16 * t + li, rows - 1);
-  f4_t acc[MT] = {};
-  for (int c = 0; c < k >> 7; ++c) {
-    const u32x4 q = *reinterpret_cast<const u32x4*>(wc + 64 * c);
-    const uint32_t s = ws[4 * c];
-    if constexpr (A4) {
-      const uint8_t* xs = reinterpret_cast<const uint8_t*>(X + (size_t)m * (k >> 1));
+    for (int j = 0; j < 4; ++j) xv[j] = x[4 * b + j];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(X + xrow[t] * (k >> 1) + 64 * c + 16 * g);
-        acc[t] = mfma_mx4(q, s, x, xs[xrow[t] * G + 4 * c + g], acc[t]);
-      }
-    } else {
-      const float scale = __builtin_bit_cast(float, s << 23);
+    for (int r = 0; r < kGemvRows; ++r) {
+      const size_t at = (size_t)min(row0 + r, n - 1) * G + b;
+      q[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(packed) + at);
+      s[r] = scales[at];
+    }
+#pragma unroll
+    for (int r = 0; r < kGemvRows; ++r) {
+      const float scale = __builtin_bit_cast(float, s[r] << 23);
+      float v = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const h8_t w = mx4_frag(q[j], scale);
+        const u32x4 w = __builtin_bit_cast(u32x4, mx4_frag(q[r][j], scale));
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          const h8_t x = *reinterpret_cast<const h8_t*>(X + 2 * (xrow[t] * k + 128 * c + 32 * g + 8 * j));
-          acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x, acc[t], 0, 0, 0);
-        }
+        for (int i = 0; i < 4; ++i) v = dot2(w[i], xv[j][i], v);
       }
+      sum[r] += b0 + lane < G ? v : 0.f;  // past the row's end: its last block again
     }
   }
-  const int col = n0 + 4 * g;
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-    if (16 * t + li < rows && col < n) store4(Y + (size_t)(m0 + 16 * t + li) * n + col, acc[t], n - col);
+  for (int r = 0; r < kGemvRows; ++r) {
+    const float v = wave_sum(sum[r]);
+    if (lane == 63) sums[part * kGemvRows + r][seg] = v;
+  }
+  __syncthreads();
+  const int row = blockIdx.x * kRows + threadIdx.x;
+  if (threadIdx.x < kRows && row < n) {
+    float v = sums[threadIdx.x][0];
+#pragma unroll
+    for (int i = 1; i < SEG; ++i) v += sums[threadIdx.x][i];
+    y[row] = (uint16_t)float_to_half_bits(v);
+  }
 }
 
-template <bool A4, bool GROUPED>
-int run(const qx_desc* d, const void* packed, const Experts& ex, int m, const void* X, uint16_t* Y, hipStream_t s) {
-  constexpr int MT = 4;
-  const long nx = ((long)d->n + 63) / 64, tiles = ((long)m + 16 * MT - 1) / (16 * MT);
-  const unsigned blocks = GROUPED ? expert_blocks(ex, m, 16 * MT, (int)nx) : nx * tiles < (1 << 22) ? (unsigned)(nx * tiles) : 0u;
-  if (blocks == 0) return QX_E_UNSUPPORTED;
-  hipLaunchKernelGGL((mx4_gemm_kernel<A4, GROUPED, MT>), dim3(blocks), dim3(256), 0, s,
-                     static_cast<const char*>(packed), static_cast<const char*>(X), Y, d->n, d->k, m, (int)nx, ex);
+template <int SEG>
+int launch_gemv_seg(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y, hipStream_t s) {
+  constexpr int kRows = kGemvRows * (kGemvWaves / SEG);
+  const long blocks = ((long)d->n + kRows - 1) / kRows;
+  if (blocks >= (1 << 22)) return QX_E_UNSUPPORTED;
+  hipLaunchKernelGGL(mx4_gemv_kernel<SEG>, dim3((unsigned)blocks), dim3(64 * kGemvWaves), 0, s,
+                     static_cast<const char*>(packed), reinterpret_cast<const u32x4*>(x), y, d->n, d->k);
   return hipGetLastError() == hipSuccess ? QX_OK : QX_E_HIP;
 }
 
 }  // namespace
 
 int launch_gemv_mx4(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y, hipStream_t s) {
-  return run<false, false>(d, packed, Experts{}, 1, x, y, s);
+  if (d->k <= 2048) return launch_gemv_seg<1>(d, packed, x, y, s);
+  if (d->k <= 4096) return launch_gemv_seg<2>(d, packed, x, y, s);
+  if (d->k <= 8192) return launch_gemv_seg<4>(d, packed, x, y, s);
+  return launch_gemv_seg<8>(d, packed, x, y, s);
 }
+
 int launch_gemm_mx4(const qx_desc* d, const void* packed, int m, const uint16_t* X, uint16_t* Y, hipStream_t s) {
-  return run<false, false>(d, packed, Experts{}, m, X, Y, s);
+  if (m == 1) return launch_gemv_mx4(d, packed, X, Y, s);
+  return mx4::launch<false, false>(d, packed, Experts{}, m, X, Y, mx4::pick_shape<false>(d->n, d->k, m, 0), s);
 }
-int launch_gemm_a4(const qx_desc* d, const void* packed, int m, const void* Xq, uint16_t* Y, hipStream_t s) {
-  return run<true, false>(d, packed, Experts{}, m, Xq, Y, s);
-}
+
 int launch_gemm_mx4_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X,
                             uint16_t* Y, hipStream_t s) {
-  return run<false, true>(d, packed, ex, m, X, Y, s);
-}
-int launch_gemm_a4_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const void* Xq,
-                           uint16_t* Y, hipStream_t s) {
-  return run<true, true>(d, packed, ex, m, Xq, Y, s);
+  return mx4::launch<false, true>(d, packed, ex, m, X, Y, mx4::pick_shape<false>(d->n, d->k, m, ex.count), s);
 }
 
 }  // namespace qx
