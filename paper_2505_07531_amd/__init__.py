@@ -311,13 +311,15 @@ def _here(stream, *tensors):
     """The raw stream, once every tensor is known to lie on the current device (a launch goes to
     the current device, whatever the tensors' own)."""
     import torch
-    at = torch.cuda.current_device()
+    at = torch._C._cuda_getDevice()
     for t in tensors:
-        if t.device.index != at:
+        if t.get_device() != at:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{at}")
-    if stream is not None and stream.device.index != at:
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(at)
+    if stream.device.index != at:
         raise ValueError(f"stream of {stream.device}, but the current device is cuda:{at}")
-    return _stream(stream)
+    return stream.cuda_stream
 
 
 def qx_quantize_mx4(m: int, k: int, X, packed, stream=None) -> None:
@@ -388,7 +390,7 @@ def quantize_mx4(X, stream=None) -> "PackedWeight":
     m, k = X.shape
     out = torch.empty(m * k // 32 * 17, dtype=torch.uint8, device=X.device)
     qx_quantize_mx4(m, k, X, out, stream)
-    return PackedWeight.from_blob(QxDesc(m, k, 4, 32, QX_MX4, 0), out)
+    return PackedWeight._around(QxDesc(m, k, 4, 32, QX_MX4, 0), out, m * k // 32 * 17)
 
 
 def quantize_a8(X, stream=None):
@@ -426,8 +428,12 @@ class PackedWeight:
     def from_blob(cls, d: QxDesc, data) -> "PackedWeight":
         """Around a blob that is in device memory already (a uint8 tensor; not copied)."""
         _chk_packed(d, data)
+        return cls._around(d, data, qx_blob_size(d))
+
+    @classmethod
+    def _around(cls, d: QxDesc, data, nbytes: int) -> "PackedWeight":
         self = cls.__new__(cls)
-        self.desc, self.nbytes, self.data = d, qx_blob_size(d), data
+        self.desc, self.nbytes, self.data = d, nbytes, data
         return self
 
     def dequant(self, out_kind: int = QX_OUT_F16, stream=None):

@@ -1,6 +1,8 @@
 // Block shapes of the MX4 products (mx4_tile.h) and the choice between them. Plain C++.
 #pragma once
 
+#include <cmath>
+
 #include "qx_internal.h"
 
 namespace qx {
@@ -44,16 +46,20 @@ inline constexpr ShapeCost shapes<true>[kShapes] = {
     {8, 4, 2, 4, 1, 2, true, {5.39f, 0.827f, 9.66f, 0.971f}},
 };
 
-// Expected cost of `tiles` row tiles of 16 * mt * wm rows by n columns.
-inline float shape_us(const ShapeCost& s, float tiles, int n, int k) {
+// Cost of `tiles` row tiles of 16 * mt * wm rows by n columns; `ragged`: their number is a guess.
+inline float shape_us(const ShapeCost& s, float tiles, int n, int k, bool ragged) {
   const long nx = ((long)n + 16 * s.nt * s.wn - 1) / (16 * s.nt * s.wn);
   const float rounds = tiles * (float)nx / 256.f, K = (float)(k / 128);
-  const float more = rounds <= 1.f ? 0.f : s.one ? (float)(long)(rounds + 0.999f) - 1.f : rounds - 1.f;
+  float more = rounds <= 1.f ? 0.f : rounds - 1.f;
+  if (s.one && more > 0.f) more = ragged ? more + 0.4f : (float)(long)(rounds + 0.999f) - 1.f;
   return s.us[0] + s.us[1] * K + more * (s.us[2] + s.us[3] * K);
 }
 
-// experts: of a grouped product (0: none). Only the device knows its sizes: the rows are taken as shared
-// evenly by as many experts as there can be, whose last tile is half full in the mean.
+// experts: of a grouped product (0: none). Only the device knows their sizes: the rows are taken as
+// shared by as many experts as there can be, with shares that differ by a factor of two or so. Then an
+// expert has half a tile more than its rows fill, and few have less than one (32 experts of
+// 4096x1408, 4001 MX4 rows: 36 us in tiles of 128 x 128, 51 in 256 x 256, which counted as one tile
+// an expert).
 template <bool A4>
 inline int pick_shape(int n, int k, int m, int experts) {
   int best = 0;
@@ -63,10 +69,10 @@ inline int pick_shape(int n, int k, int m, int experts) {
     const int bm = 16 * s.mt * s.wm;
     float tiles = (float)((m + bm - 1) / bm);
     if (experts > 0) {
-      const float used = (float)(experts < m ? experts : m), each = (float)m / used / (float)bm + 0.5f;
-      tiles = used * (each > 1.f ? each : 1.f);
+      const float used = (float)(experts < m ? experts : m), full = (float)m / (used * (float)bm);
+      tiles = used * (0.5f + full + 0.5f * std::exp(-2.f * full));
     }
-    const float us = shape_us(s, tiles, n, k);
+    const float us = shape_us(s, tiles, n, k, experts > 0);
     if (us < least) least = us, best = i;
   }
   return best;

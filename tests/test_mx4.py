@@ -165,8 +165,7 @@ class _Fake:
     def is_contiguous(self):
         return self._c
 
-    @property
-    def device(self):
+    def get_device(self):
         raise AssertionError("past the checks: the call would have launched")
 
     def data_ptr(self):
@@ -207,12 +206,14 @@ def test_binding_checks_tensors():
 
 def test_tensors_of_another_device_are_refused(monkeypatch):
     """A launch goes to the current device: tensors, or a stream, of another one are an error."""
-    import types
+    from types import SimpleNamespace as NS
     torch = pytest.importorskip("torch")
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    here, there = (types.SimpleNamespace(device=types.SimpleNamespace(index=i)) for i in (0, 1))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 5, raising=False)
+    here, there = (NS(get_device=lambda i=i: i, device=NS(index=i), cuda_stream=7 + i) for i in (0, 1))
     with pytest.raises(ValueError):
         qx._here(None, here, there)
     with pytest.raises(ValueError):
         qx._here(there, here, here)
-    assert qx._here(types.SimpleNamespace(device=here.device, cuda_stream=7), here, here) == 7
+    assert qx._here(here, here, here) == 7
+    assert qx._here(None, here) == 5
