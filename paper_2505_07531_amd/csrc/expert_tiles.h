@@ -37,13 +37,14 @@ __device__ __forceinline__ ExpertTile expert_tile(const Experts& ex, int m, int 
     scan(e0);
     total += __builtin_amdgcn_readlane(sum, 63);
   }
+  total = min(total, (1 << 30) / nx);  // more than any launch has: overlapping offsets
   const int share = (total * nx + 7) >> 3, at = (block & 7) * share + (block >> 3);
   ExpertTile r = {0, 0, 0, 0};
   if ((block >> 3) >= share || at >= total * nx) return r;
   int before = 0;
   for (int e0 = 0; e0 < ex.count; e0 += 64) {
     if (ex.count > 64) scan(e0);
-    const unsigned long long past = __ballot((before + sum) * nx > at);
+    const unsigned long long past = __ballot(before + sum > at / nx);
     if (past != 0) {
       const int f = __builtin_ctzll(past), tiles = __builtin_amdgcn_readlane(own, f);
       const int in = at - (before + __builtin_amdgcn_readlane(sum, f) - tiles) * nx, mt = in % tiles;

@@ -13,6 +13,7 @@ import oracle
 from oracle import mx4
 import qx_inputs as qi
 from helpers import activations, random_quant, to_dev
+from test_mx4_plan import shape_cases
 
 pytestmark = pytest.mark.gpu
 
@@ -295,6 +296,45 @@ def test_grouped_one_expert_is_gemm(gpu):
     pe, ws = experts_of(gpu, 4, 3, 32, 130, 640, 1, 2)
     x = activations(640, 6, 50)
     check(run_grouped(gpu, pe, x, [0, 50]), x, ws[0])
+
+
+@pytest.mark.parametrize("a4,shape,n,k,m,experts", shape_cases())
+def test_every_block_shape(gpu, a4, shape, n, k, m, experts):
+    """Every shape of the tiles, alone or grouped (test_mx4_plan shows which product takes which)."""
+    if experts:
+        rng = np.random.default_rng(n + m)
+        off = np.concatenate([[0], np.sort(rng.integers(0, m + 1, experts - 1)), [m]])
+        pe, ws = experts_of(gpu, 4, 3, 32, n, k, experts, 7)
+        x = activations(k, 3, m)
+        check_grouped(run_grouped(gpu, pe, x, off, a4=bool(a4)), mx4.levels(*mx4.quantize(x)) if a4 else x, ws, off, 0x5A5A)
+        return
+    q = random_mx4(n, k, 7)
+    x = activations(k, 3, m)
+    pw = gpu.PackedWeight.from_quant(q)
+    if a4:
+        check(pw.gemm_a4(gpu.quantize_mx4(to_dev(x))).cpu().numpy(), mx4.levels(*mx4.quantize(x)), mx4.levels(q.codes, q.scales))
+    else:
+        check(pw.gemm(to_dev(x)).cpu().numpy(), x, mx4.dequant(q.codes, q.scales))
+
+
+@pytest.mark.parametrize("a4", [False, True])
+@pytest.mark.parametrize("seed", range(6))
+def test_grouped_random_offsets(gpu, a4, seed):
+    """Many experts of one small matrix each, any number of rows of any of them."""
+    rng = np.random.default_rng(seed)
+    experts, n, k = int(rng.integers(1, 1025)), 19, 128
+    count = rng.integers(0, 40, experts) * (rng.random(experts) < rng.choice([0.05, 0.5, 1.0]))
+    off = np.concatenate([[0], np.cumsum(count)]) + rng.integers(0, 5)
+    m = int(off[-1]) + int(rng.integers(0, 5))
+    q = random_mx4(n * experts, k, seed)
+    size = mx4.packed_size(n, k)
+    blobs = np.stack([mx4.pack(q.codes[e * n:(e + 1) * n], q.scales[e * n:(e + 1) * n]) for e in range(experts)])
+    data = np.zeros((experts, (size + 15) // 16 * 16), np.uint8)
+    data[:, :size] = blobs
+    pe = gpu.PackedExperts(gpu.desc(n, k, 4, 32, gpu.QX_MX4), to_dev(data))
+    ws = mx4.dequant(q.codes, q.scales).reshape(experts, n, k)
+    x = activations(k, seed, m)
+    check_grouped(run_grouped(gpu, pe, x, off, a4=a4), mx4.levels(*mx4.quantize(x)) if a4 else x, ws, off, 0x5A5A)
 
 
 # ------------------------------------------------------------------ as they are used
