@@ -16,7 +16,7 @@ OBJDIR = os.path.join(ROOT, "_build")
 
 SOURCES = ["qx_api.cpp", "dequant.hip", "gemv.hip", "gemv_a8.hip", "gemv_lut_a8.hip", "gemv_multi.hip",
            "gemm.hip", "gemm_a8.hip", "gemm_tile.hip", "gemm_skinny.hip", "qx_api_mx4.cpp",
-           "mx4_convert.hip", "mx4_gemm.hip", "mx4_gemm_a4.hip"]
+           "mx4_convert.hip", "mx4_gemm.hip", "mx4_gemm_a4.hip", "grouped.hip"]
 PROBE_SOURCES = ["bw_probe.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc" if os.path.exists("/opt/rocm/bin/hipcc") else "hipcc")

@@ -551,11 +551,11 @@ int run(const qx_desc* d, const void* packed, int m, const void* X, const float*
   }
 }
 
-// Products grouped by expert, of fp16 rows: shape S.
-template <int BITS, int KIND, int G, int S>
+// fp16 rows grouped by expert, shape C.
+template <int BITS, int KIND, int G>
 int launch_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X, uint16_t* Y,
                    hipStream_t s) {
-  constexpr ShapeCost C = kShape[S];
+  constexpr ShapeCost C = kShape[kC];
   using TS = TileShape<BITS, KIND, G, C.mt, C.nt, C.wm, C.sc, C.ks>;
   static_assert(TS::kLds <= kLdsBytes, "LDS");
   const int nx = (int)(((long)d->n + TS::BN - 1) / TS::BN);
@@ -584,17 +584,8 @@ int launch_gemm_tile(const qx_desc* d, const void* packed, int m, const void* X,
 
 int launch_gemm_tile_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X,
                              uint16_t* Y, hipStream_t s) {
-  // Rows of an expert, were they shared evenly (us in H / E / C; 32 experts of 2816x4096, m = 32; 8 of
-  // 1376x4096, m = 999; 8 of 4096x4096, m = 4000; unevenly shared): uniform-4 g128 48 / 57 / 111, 46 / 40 / 70,
-  // 603 / 213 / 185; codebook-3 g128 48 / 51 / 100, 44 / 39 / 67, 572 / 202 / 180. The 4-bit codebooks, whose
-  // tables H reads for every 32 columns, leave it earlier (g64: 76 / 78 / 127; 8 of 5865x2816, m = 70, 60 / 55 / 60).
-  const long each = m / ex.count;
-  const bool few = each <= (d->kind == QX_CODEBOOK && d->bits == 4 ? 4 : 32), many = each >= 300;
-#define QX_TILE_GROUPED(B, K, G)                                                     \
-  if (d->bits == B && d->kind == K && d->group == G)                                 \
-    return few    ? launch_grouped<B, K, G, kH>(d, packed, ex, m, X, Y, s)           \
-           : many ? launch_grouped<B, K, G, kC>(d, packed, ex, m, X, Y, s)           \
-                  : launch_grouped<B, K, G, kE>(d, packed, ex, m, X, Y, s);
+#define QX_TILE_GROUPED(B, K, G) \
+  if (d->bits == B && d->kind == K && d->group == G) return launch_grouped<B, K, G>(d, packed, ex, m, X, Y, s);
   QX_TILE_FORMATS(QX_TILE_GROUPED)
 #undef QX_TILE_GROUPED
   return QX_E_UNSUPPORTED;

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "expert_tiles.h"
+#include "lds_loads.h"
 #include "qx_device.h"
 
 namespace qx {
@@ -23,22 +24,6 @@ __device__ __forceinline__ f4_t mfma_mx4(u32x4 a, uint32_t sa, u32x4 b, uint32_t
   const i32x8 av = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
   const i32x8 bv = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 4, 4, 0, (int)sa, 0, (int)sb);
-}
-
-// Neighbouring columns of a row of Y, which may start at any multiple of 2 bytes.
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-__device__ __forceinline__ void store4(uint16_t* dst, f4_t v, int left) {  // left: columns to the row's end
-  uint32_t h[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r) h[r] = float_to_half_bits(v[r]);
-  if (left >= 4) {
-    *reinterpret_cast<u32x2_any*>(dst) = u32x2{h[0] | (h[1] << 16), h[2] | (h[3] << 16)};
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (r < left) dst[r] = (uint16_t)h[r];
-  }
 }
 
 }  // namespace qx

@@ -55,11 +55,17 @@ inline float shape_us(const ShapeCost& s, float tiles, int n, int k, bool ragged
   return s.us[0] + s.us[1] * K + more * (s.us[2] + s.us[3] * K);
 }
 
-// experts: of a grouped product (0: none). Only the device knows their sizes: the rows are taken as
-// shared by as many experts as there can be, with shares that differ by a factor of two or so. Then an
-// expert has half a tile more than its rows fill, and few have less than one (32 experts of
+// Row tiles of bm rows that m rows of `experts` experts take. Only the device knows their sizes: the rows
+// are taken as shared by as many experts as there can be, with shares that differ by a factor of two or
+// so. Then an expert has half a tile more than its rows fill, and few have less than one (32 experts of
 // 4096x1408, 4001 MX4 rows: 36 us in tiles of 128 x 128, 51 in 256 x 256, which counted as one tile
 // an expert).
+inline float expert_tiles(int m, int experts, int bm) {
+  const float used = (float)(experts < m ? experts : m), full = (float)m / (used * (float)bm);
+  return used * (0.5f + full + 0.5f * std::exp(-2.f * full));
+}
+
+// experts: of a grouped product (0: none).
 template <bool A4>
 inline int pick_shape(int n, int k, int m, int experts) {
   int best = 0;
@@ -67,11 +73,7 @@ inline int pick_shape(int n, int k, int m, int experts) {
   for (int i = 0; i < kShapes; ++i) {
     const ShapeCost& s = shapes<A4>[i];
     const int bm = 16 * s.mt * s.wm;
-    float tiles = (float)((m + bm - 1) / bm);
-    if (experts > 0) {
-      const float used = (float)(experts < m ? experts : m), full = (float)m / (used * (float)bm);
-      tiles = used * (0.5f + full + 0.5f * std::exp(-2.f * full));
-    }
+    const float tiles = experts > 0 ? expert_tiles(m, experts, bm) : (float)((m + bm - 1) / bm);
     const float us = shape_us(s, tiles, n, k, experts > 0);
     if (us < least) least = us, best = i;
   }

@@ -27,24 +27,12 @@
 #pragma once
 
 #include "gemm_tile_plan.h"
+#include "lds_loads.h"
 #include "mx4_device.h"
 #include "mx4_plan.h"
 
 namespace qx {
 namespace mx4 {
-
-typedef __attribute__((address_space(1))) const void GlobalVoid;
-typedef __attribute__((address_space(3))) void LdsVoid;
-
-// SIZE bytes a lane from memory straight to LDS: lane l's go to dst + SIZE * l (dst uniform).
-template <int SIZE>
-__device__ __forceinline__ void load_lds(const char* src, char* dst) {
-  static_assert(SIZE == 16 || SIZE == 4, "sizes that the target has");
-  if constexpr (SIZE == 16)
-    __builtin_amdgcn_global_load_lds((GlobalVoid*)src, (LdsVoid*)dst, 16, 0, 0);
-  else
-    __builtin_amdgcn_global_load_lds((GlobalVoid*)src, (LdsVoid*)dst, 4, 0, 0);
-}
 
 template <bool A4_, int I>
 struct Mx4Shape {

@@ -70,7 +70,7 @@ int qx_gemm_grouped(const qx_desc* d, const void* packed, size_t stride, int32_t
   if (!aligned16(packed) || !aligned16(X) || !aligned4(offsets) || !aligned2(Y)) return QX_E_ARG;
   const Experts ex = {stride, experts, offsets};
   if (d->kind == QX_MX4) return launch_gemm_mx4_grouped(d, packed, ex, m, X, Y, stream);
-  return launch_gemm_tile_grouped(d, packed, ex, m, X, Y, stream);
+  return launch_gemm_grouped(d, packed, ex, m, X, Y, stream);
 }
 
 int qx_gemm_a4_grouped(const qx_desc* d, const void* packed, size_t stride, int32_t experts, int32_t m,

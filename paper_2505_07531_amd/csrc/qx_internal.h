@@ -105,7 +105,10 @@ int launch_gemm_mx4_grouped(const qx_desc* d, const void* packed, const Experts&
                             uint16_t* Y, hipStream_t s);
 int launch_gemm_a4_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const void* Xq,
                            uint16_t* Y, hipStream_t s);
-// fp16 rows grouped by expert, the other kinds (gemm_tile.hip).
+// fp16 rows grouped by expert, the other kinds: grouped.hip, and for experts of many rows the 128 x 192
+// tiles of gemm_tile.hip.
+int launch_gemm_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X, uint16_t* Y,
+                        hipStream_t s);
 int launch_gemm_tile_grouped(const qx_desc* d, const void* packed, const Experts& ex, int m, const uint16_t* X,
                              uint16_t* Y, hipStream_t s);
 
