@@ -11,40 +11,51 @@ namespace mx4 {
 // A block of wm x wn x wk waves, each with mt x nt tiles of 16 x 16 (activation rows x weight rows);
 // the wk waves take different k, ks units of it (128 with MX4 rows, 64 with fp16) a stage.
 // Cost in us at k = 128 K of up to 256 blocks, one a compute unit: us[0] + us[1] K; of every 256 more:
-// us[2] + us[3] K. One block of a shape with `one` set fills a compute unit, so that those are whole
-// rounds. Fitted to 2577 times (170 sizes with n = 256 to 22016, k = 512 to 11264, m = 1 to 4096), of which
-// 96 of 100 are within 13 % (fp16 rows; MX4 rows within 30 %); the shapes that they choose take 0.7 % and
-// 3 % more than the best of the measured ones in the mean.
+// us[2] + us[3] K. One block of a shape with `one` set fills a compute unit, or nearly: those come in
+// whole rounds. Fitted to the times of 384 products (168 of one matrix, n = 256 to 22016, k = 512 to 11264,
+// m = 2 to 4096, and 216 of 4 to 128 experts, weights read from memory); where a shape is within 30 % of
+// the best, 96 of 100 are within 22 % (fp16 rows) and 27 % (MX4 rows). The shapes that they choose take 0.9
+// and 1.2 % more than the best of the measured ones in the mean, 2.9 and 2.0 % grouped by expert, where the
+// rows of an expert are a guess.
+// The last shape has several blocks a compute unit, for experts with few rows (32 experts of 2816x4096, 32
+// fp16 rows: 19.9 us, 24.7 in the best of the others; 64 of 2816x2048, 48 MX4 rows: 16.6, 18.4).
 struct ShapeCost {
   int mt, nt, wm, wn, wk, ks;
   bool one;
   float us[4];
 };
-constexpr int kShapes = 9;
+constexpr int kShapes = 10;
 template <bool A4>
 inline constexpr ShapeCost shapes[kShapes] = {
-    {1, 1, 1, 1, 8, 2, true, {2.92f, 0.0693f, 1.54f, 0.0845f}},
-    {1, 2, 1, 1, 4, 2, false, {2.7f, 0.149f, 0.374f, 0.0869f}},
-    {2, 2, 1, 1, 8, 1, true, {3.16f, 0.136f, 1.8f, 0.162f}},
-    {2, 4, 1, 1, 4, 1, false, {3.2f, 0.281f, 1.27f, 0.15f}},
-    {4, 2, 1, 1, 8, 1, true, {3.63f, 0.211f, 2.41f, 0.253f}},
-    {4, 2, 1, 2, 4, 1, true, {3.65f, 0.323f, 2.67f, 0.366f}},
-    {4, 4, 1, 2, 2, 1, false, {4.14f, 0.711f, 2.11f, 0.499f}},
-    {4, 4, 2, 4, 1, 1, true, {4.33f, 1.6f, 4.51f, 1.62f}},
-    {8, 4, 2, 4, 1, 1, true, {5.73f, 2.61f, 11.3f, 2.62f}},
+    {1, 1, 1, 1, 8, 2, true, {3.33f, 0.0665f, 1.44f, 0.102f}},
+    {1, 2, 1, 1, 4, 2, false, {2.89f, 0.159f, 0.519f, 0.102f}},
+    {2, 2, 1, 1, 8, 1, true, {3.46f, 0.137f, 1.82f, 0.194f}},
+    {2, 4, 1, 1, 4, 1, false, {3.19f, 0.314f, 0.733f, 0.215f}},
+    {4, 2, 1, 1, 8, 1, true, {3.8f, 0.229f, 2.35f, 0.288f}},
+    {4, 2, 1, 2, 4, 1, true, {3.79f, 0.35f, 2.76f, 0.409f}},
+    {4, 4, 1, 2, 2, 1, false, {4.41f, 0.787f, 1.87f, 0.539f}},
+    {4, 4, 2, 4, 1, 1, true, {5.15f, 1.73f, 5.32f, 1.79f}},
+    {8, 4, 2, 4, 1, 1, true, {8.29f, 2.66f, 4.93f, 2.95f}},
+    {1, 4, 1, 1, 4, 1, false, {2.8f, 0.273f, 0.459f, 0.169f}},
 };
 template <>
 inline constexpr ShapeCost shapes<true>[kShapes] = {
-    {1, 1, 1, 1, 8, 2, false, {3.04f, 0.0253f, 0.792f, 0.0301f}},
-    {1, 2, 1, 1, 4, 2, false, {2.85f, 0.0567f, 0.353f, 0.0504f}},
-    {2, 2, 1, 1, 8, 1, false, {3.35f, 0.05f, 0.826f, 0.0711f}},
-    {2, 4, 1, 1, 4, 1, false, {3.35f, 0.104f, 0.258f, 0.113f}},
-    {4, 2, 1, 1, 8, 1, true, {3.85f, 0.068f, 2.15f, 0.0984f}},
-    {4, 4, 1, 1, 4, 1, false, {4.1f, 0.144f, 1.68f, 0.123f}},
-    {4, 4, 1, 1, 8, 1, true, {4.31f, 0.107f, 3.25f, 0.133f}},
-    {4, 4, 2, 2, 1, 2, false, {4.43f, 0.411f, 2.28f, 0.333f}},
-    {8, 4, 2, 4, 1, 2, true, {5.39f, 0.827f, 9.66f, 0.971f}},
+    {1, 1, 1, 1, 8, 2, false, {3.17f, 0.0293f, 0.906f, 0.0424f}},
+    {1, 2, 1, 1, 4, 2, false, {2.96f, 0.0658f, 0.535f, 0.0673f}},
+    {2, 2, 1, 1, 8, 1, false, {3.47f, 0.06f, 0.963f, 0.0944f}},
+    {2, 4, 1, 1, 4, 1, true, {3.27f, 0.132f, 0.683f, 0.138f}},
+    {4, 2, 1, 1, 8, 1, true, {3.75f, 0.084f, 2.14f, 0.144f}},
+    {4, 4, 1, 1, 4, 1, true, {4.07f, 0.169f, 1.58f, 0.154f}},
+    {4, 4, 1, 1, 8, 1, true, {4.5f, 0.129f, 3.31f, 0.198f}},
+    {4, 4, 2, 2, 1, 2, true, {5.1f, 0.437f, 2.1f, 0.317f}},
+    {8, 4, 2, 4, 1, 2, true, {6.73f, 0.981f, 5.95f, 1.15f}},
+    {1, 2, 1, 1, 4, 1, true, {2.66f, 0.0883f, 0.285f, 0.0631f}},
 };
+// fp16 rows of one matrix do without the last shape: it is the best for 6 of the 168 products, by 4 to 19 %,
+// but a cost is too coarse to tell them from those where its blocks come out uneven over the compute units
+// (19088x7168, m = 2: 25.7 us, 19.1 in 16 x 32).
+template <bool A4>
+constexpr bool built(int shape, bool grouped) { return A4 || grouped || shape < kShapes - 1; }
 
 // Cost of `tiles` row tiles of 16 * mt * wm rows by n columns; `ragged`: their number is a guess.
 inline float shape_us(const ShapeCost& s, float tiles, int n, int k, bool ragged) {
@@ -71,6 +82,7 @@ inline int pick_shape(int n, int k, int m, int experts) {
   int best = 0;
   float least = 1e30f;
   for (int i = 0; i < kShapes; ++i) {
+    if (!built<A4>(i, experts > 0)) continue;
     const ShapeCost& s = shapes<A4>[i];
     const int bm = 16 * s.mt * s.wm;
     const float tiles = experts > 0 ? expert_tiles(m, experts, bm) : (float)((m + bm - 1) / bm);

@@ -89,7 +89,7 @@ template <class S>
 struct Mx4Loads {
   const char *W, *Wsc, *X, *Xsc;  // the block's first rows: codes (or fp16) and scales
   unsigned wat[S::WL], xat[S::XL];  // this thread's loads, from there
-  int C, G, wave, t, wlast, xlast;
+  int C, G, wave, t, wlast, xlast, xloads;
 
   __device__ __forceinline__ Mx4Loads(const char* packed, const char* Xall, const Mx4Block& b, int n, int k, int m) {
     const int wbytes = k >> 1, xbytes = S::A4 ? k >> 1 : k * 2;  // of a row
@@ -100,6 +100,10 @@ struct Mx4Loads {
     Xsc = S::A4 ? Xall + (size_t)m * xbytes + (size_t)b.m0 * G : nullptr;
     C = k / S::UK, t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     wlast = min(n - b.n0, S::BN) - 1, xlast = b.rows - 1;
+    // Of a block with few rows a wave leaves out the loads past the last one: what LDS holds there enters
+    // columns of products that are not stored (32 experts, 32 fp16 rows: 28.4 to 25.8 us; of the blocks
+    // of 64 rows and more none was faster for it, 11008x4096 m = 2001 183.5 to 192).
+    xloads = (b.rows * S::XP - wave * 64 + S::kThreads - 1) / S::kThreads;
 #pragma unroll
     for (int i = 0; i < S::WL; ++i) {
       const int q = i * S::kThreads + t, row = q / S::WP, p = (q % S::WP) ^ swizzle<S::WP>(row);
@@ -126,7 +130,8 @@ struct Mx4Loads {
 #pragma unroll
     for (int i = 0; i < S::WL; ++i) load_lds<16>(wb + wat[i], buf + (i * S::kThreads + wave * 64) * 16);
 #pragma unroll
-    for (int i = 0; i < S::XL; ++i) load_lds<16>(xb + xat[i], buf + S::kW + (i * S::kThreads + wave * 64) * 16);
+    for (int i = 0; i < S::XL; ++i)
+      if (S::BM > 32 || i < xloads) load_lds<16>(xb + xat[i], buf + S::kW + (i * S::kThreads + wave * 64) * 16);
   }
 
   // Where the 16 bytes of a row's scales numbered p begin: the last ones end with the row.
@@ -377,8 +382,9 @@ template <bool A4, bool GROUPED, int I = 0>
 int launch(const qx_desc* d, const void* packed, const Experts& ex, int m, const void* X, uint16_t* Y, int shape,
            hipStream_t s) {
   if constexpr (I < kShapes) {
-    return shape == I ? launch_shape<Mx4Shape<A4, I>, GROUPED>(d, packed, ex, m, X, Y, s)
-                      : launch<A4, GROUPED, I + 1>(d, packed, ex, m, X, Y, shape, s);
+    if constexpr (built<A4>(I, GROUPED))
+      if (shape == I) return launch_shape<Mx4Shape<A4, I>, GROUPED>(d, packed, ex, m, X, Y, s);
+    return launch<A4, GROUPED, I + 1>(d, packed, ex, m, X, Y, shape, s);
   }
   return QX_E_UNSUPPORTED;
 }
