@@ -1,5 +1,18 @@
 // Products grouped by expert, fp16 rows, for the uniform, codebook and Q4X kinds: Y[r] = X[r] W'[e]^T for
 // the rows r of expert e, in tiles (expert_tiles.h finds a block's expert and rows from the offsets).
+//
+// W' are the fp16 weights that qx_dequant writes: uniform s (q - z), the difference exact, the product
+// rounded once; codebooks two byte lookups a code; Q4X a lookup times s, rounded once. Codes are decoded in
+// registers in the order of k, 8 a lane, so that rows of X go to LDS as they are; the products are
+// v_mfma_f32_16x16x32_f16 with fp32 sums, weights first: a lane ends with four columns of Y.
+//
+// Experts have few rows each, so a tile is small and its time is that of one block's chain over k: codes,
+// tables and rows go straight to LDS a stage ahead, one barrier a stage, and k is split over the waves of a
+// block, whose sums are added in their order. A piece of codes is 16 bytes of a chunk and slice; the chunks of
+// a stage lie beside each other, 32 to 64 bytes a slice, which is what the loads cost most by: a stage of two
+// chunks takes 1.7 us of loads and 1.65 us of decoding and products without each other, 2.1 together (8 experts
+// of 1376x4096, uniform-4 g128, m = 999, 64 x 128: 27, 26.5 and 33.7 us). Measured: 30 us there (375 TFLOP/s),
+// 39 with the kernel of the single product; 32 experts, m = 64: 24 us, 90 MB of weights at 3.8 TB/s.
 #include "expert_tiles.h"
 #include "grouped_plan.h"
 #include "lds_loads.h"
@@ -117,13 +130,17 @@ __global__ __launch_bounds__(THREADS, THREADS / 256) void grouped_kernel(const c
     if (KIND == QX_UNIFORM) mat[i] = (min(row, wlast) * G_row + cc * NG + w) * 4;
     else mat[i] = w == 0 ? (min(row, wlast) * G_row + cc * 2) * 2 : min(row, wlast) * words * 4;  // selectors: of the row
   }
+  // of a block with few rows a wave leaves out the loads past the last one: what LDS holds there enters
+  // columns of products that are not stored
+  const int xloads = (own.rows * 16 * KU - wave * 64 + NTH - 1) / NTH;
   auto load = [&](int st, char* buf) {
     const int c = first(st);
     // kept apart from the lanes' offsets: summed before the loop they would take two registers each
     const char *xb = X + c * 256, *wb = codes + c * 16, *tb = tables + c * (KIND == QX_UNIFORM ? NG * 4 : KIND == QX_Q4X ? 4 : S::kParts * 16);
     asm volatile("" : "+s"(xb), "+s"(wb), "+s"(tb));
 #pragma unroll
-    for (int i = 0; i < S::loads(S::kXPieces); ++i) load_lds<16>(xb + xat[i], buf + S::kX + (i * NTH + wave * 64) * 16);
+    for (int i = 0; i < S::loads(S::kXPieces); ++i)
+      if (S::BM > 32 || i < xloads) load_lds<16>(xb + xat[i], buf + S::kX + (i * NTH + wave * 64) * 16);
 #pragma unroll
     for (int i = 0; i < S::loads(S::kWPieces); ++i) load_lds<16>(wb + wat[i], buf + S::kW + (i * NTH + wave * 64) * 16);
 #pragma unroll
@@ -289,7 +306,8 @@ int launch_gemm_grouped(const qx_desc* d, const void* packed, const Experts& ex,
     return shape == 0   ? launch_shape<B, K, G, 0>(d, packed, ex, m, X, Y, s)        \
            : shape == 1 ? launch_shape<B, K, G, 1>(d, packed, ex, m, X, Y, s)        \
            : shape == 2 ? launch_shape<B, K, G, 2>(d, packed, ex, m, X, Y, s)        \
-                        : launch_shape<B, K, G, 3>(d, packed, ex, m, X, Y, s);
+           : shape == 3 ? launch_shape<B, K, G, 3>(d, packed, ex, m, X, Y, s)        \
+                        : launch_shape<B, K, G, 4>(d, packed, ex, m, X, Y, s);
   QX_GROUPED(3, 0, 32) QX_GROUPED(3, 0, 64) QX_GROUPED(3, 0, 128) QX_GROUPED(3, 1, 32) QX_GROUPED(3, 1, 64)
   QX_GROUPED(3, 1, 128) QX_GROUPED(4, 0, 32) QX_GROUPED(4, 0, 64) QX_GROUPED(4, 0, 128) QX_GROUPED(4, 1, 32)
   QX_GROUPED(4, 1, 64) QX_GROUPED(4, 1, 128) QX_GROUPED(4, 2, 64)

@@ -7,29 +7,33 @@
 namespace qx {
 namespace grouped {
 
-// The first four are those of grouped.hip, ks chunks a stage; the last one is shape C of gemm_tile.hip
-// (128 x 192). Costs as in mx4_plan.h, fitted to 1170 times (8 and 32 experts of 1376x4096, 4096x1408 and
-// 2816x2048, 2 to 350 rows each, unevenly shared), half of them within 5 to 12 %: of uniform-4 g128 and
-// uniform-3 g64, and of codebook-4 g64, whose table reads fill LDS. The shapes that they choose take 1.3 %
-// and 3.7 % more than the best in the mean. us of the five with uniform-4 g128: 32 experts of 1376x4096,
-// m = 64 24 / 33 / 56 / 50 / 67, m = 960 54 / 44 / 59 / 56 / 71, m = 11200 490 / 310 / 253 / 238 / 201; 8 of
-// 2816x2048, m = 512 31 / 23 / 18 / 21 / 37; 32 of 2816x2048, m = 4160 212 / 122 / 115 / 98 / 111.
-constexpr int kShapes = 5, kTile = 4;
+// The last shape is C of gemm_tile.hip (128 x 192), the others are those of grouped.hip, ks chunks a stage.
+// Costs as in mx4_plan.h, fitted to the times of 181 sizes (4 to 128 experts, n = 256 to 6000, k = 512 to 5120,
+// 1 to 300 rows each, unevenly shared, weights read from memory): of uniform-4 g128, uniform-3 g64 and
+// codebook-3 g128, and of codebook-4 g64, whose table reads fill LDS. Where a shape is within 30 % of the
+// best, 96 of 100 are within 25 %; the shapes that they choose take 3.9 and 2.4 % more than the best in the
+// mean. us in the order of the list, uniform-4 g128: 8 experts of 576x3584, m = 108 8.0 / 12.0 / 13.2 / 24 / 28;
+// 66 of 694x1024, m = 940 17 / 13 / 16 / 22 / 18; 5 of 916x3840, m = 361 (from the third on) 15 / 26 / 30 / 62; 7 of
+// 2057x2688, m = 402 29 / 25 / 24 / 22 / 25 / 47; 78 of 3398x768, m = 3471 205 / 107 / 83 / 104 / 65 / 87; 5 of
+// 5205x3712, m = 808 (from the third on) 92 / 95 / 94 / 70.
+constexpr int kShapes = 6, kTile = 5;
 using mx4::ShapeCost;
 inline constexpr ShapeCost shapes[2][kShapes] = {
     {
-        {1, 2, 1, 1, 4, 4, false, {1.56f, 0.266f, 0.703f, 0.103f}},
-        {2, 2, 1, 2, 2, 2, false, {2.69f, 0.478f, 0.803f, 0.261f}},
-        {4, 2, 1, 4, 2, 2, true, {3.f, 0.809f, 2.8f, 0.939f}},
-        {4, 2, 1, 4, 1, 1, false, {3.8f, 1.02f, 0.274f, 1.f}},
-        {8, 3, 1, 4, 2, 2, true, {8.43f, 1.7f, 14.9f, 0.943f}},
+        {1, 2, 1, 1, 4, 4, false, {3.62f, 0.193f, 0.486f, 0.139f}},
+        {1, 2, 1, 2, 2, 2, false, {3.21f, 0.404f, 0.2f, 0.293f}},
+        {2, 2, 1, 2, 2, 2, false, {3.67f, 0.434f, 0.439f, 0.345f}},
+        {4, 2, 1, 4, 2, 2, true, {4.15f, 0.93f, 3.38f, 1.03f}},
+        {4, 2, 1, 4, 1, 1, true, {3.07f, 1.14f, 0.2f, 0.953f}},
+        {8, 3, 1, 4, 2, 2, true, {5.78f, 2.12f, 0.2f, 2.06f}},
     },
     {
-        {1, 2, 1, 1, 4, 4, false, {3.5f, 0.285f, 1.15f, 0.141f}},
-        {2, 2, 1, 2, 2, 2, false, {3.37f, 0.615f, 1.5f, 0.338f}},
-        {4, 2, 1, 4, 2, 2, true, {3.f, 1.02f, 4.85f, 0.976f}},
-        {4, 2, 1, 4, 1, 1, false, {6.14f, 1.15f, 2.17f, 1.16f}},
-        {8, 3, 1, 4, 2, 2, true, {10.5f, 2.08f, 24.f, 0.885f}},
+        {1, 2, 1, 1, 4, 4, true, {3.54f, 0.216f, 0.704f, 0.201f}},
+        {1, 2, 1, 2, 2, 2, true, {3.3f, 0.453f, 0.2f, 0.438f}},
+        {2, 2, 1, 2, 2, 2, true, {3.72f, 0.483f, 0.657f, 0.47f}},
+        {4, 2, 1, 4, 2, 2, true, {4.62f, 1.14f, 4.32f, 1.22f}},
+        {4, 2, 1, 4, 1, 1, true, {2.89f, 1.36f, 0.386f, 1.33f}},
+        {8, 3, 1, 4, 2, 2, true, {5.85f, 2.61f, 1.71f, 2.61f}},
     },
 };
 
