@@ -200,7 +200,8 @@ int qx_dequant(const qx_desc* d, const void* packed, int out_kind, void* out, hi
  * result is deterministic run to run. Uniform groups are multiplied with their
  * exact levels s*(q - z), the zero point taken out once per group, rather than
  * with W' rounded to binary16: the two differ by that rounding (at most 2^-12
- * of each weight). n = 0 is a no-op.
+ * of each weight). n = 0 is a no-op. MX4: W' itself; QX_E_UNSUPPORTED for more
+ * rows than one launch takes (4194304 blocks of 4 to 32 rows).
  */
 int qx_gemv(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y,
             hipStream_t stream);
@@ -276,7 +277,9 @@ int qx_gemm_a8(const qx_desc* d, const void* packed, int32_t m, const int8_t* Xq
  *   rows, m <= 48 by shape and format, each lane decoding its own chunks as in
  *   the GEMV), or, for m <= 4 where that measured faster, GEMV-style with every
  *   code decoded once for all rows. m = 0 or n = 0 is a no-op; m must be
- *   <= 65536. All formats, Q4X and MX4 included. Deterministic.
+ *   <= 65536. All formats, Q4X and MX4 included. Deterministic. MX4:
+ *   QX_E_UNSUPPORTED when m rows by n columns are more tiles than one launch
+ *   takes (4194304).
  */
 int qx_gemm(const qx_desc* d, const void* packed, int32_t m, const uint16_t* X, uint16_t* Y,
             hipStream_t stream);
@@ -290,7 +293,8 @@ int qx_gemm(const qx_desc* d, const void* packed, int32_t m, const uint16_t* X, 
  *           to nearest-even from fp32 sums of exact products
  *           value * value * 2^(e_w - 127) * 2^(e_x - 127) (scales are not
  *           rounded to fp16 here; a scale of 255 on either side gives NaN).
- * m = 0 or n = 0 is a no-op; m must be <= 65536. Deterministic.
+ * m = 0 or n = 0 is a no-op; m must be <= 65536. QX_E_UNSUPPORTED for more
+ * tiles than one launch takes (4194304). Deterministic.
  */
 int qx_gemm_a4(const qx_desc* d, const void* packed, int32_t m, const void* Xq, uint16_t* Y, hipStream_t stream);
 
@@ -299,7 +303,7 @@ int qx_gemm_a4(const qx_desc* d, const void* packed, int32_t m, const void* Xq, 
  *   d        descriptor of each expert's matrix.
  *   packed   the experts' blobs, that of expert e at byte e * stride; stride a
  *            multiple of 16, at least the blob's size. 0 <= experts <= 1024.
- *   offsets  device, int32 [experts + 1], not decreasing: rows offsets[e] ..
+ *   offsets  device, int32 [experts + 1] (4-byte aligned), not decreasing: rows offsets[e] ..
  *            offsets[e+1] - 1 of X belong to expert e. It is read when the
  *            work runs, so a router's output needs no copy to the host.
  *   X, Y     fp16 [m][k] and [m][n] as for qx_gemm. Rows outside of

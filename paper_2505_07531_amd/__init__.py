@@ -255,8 +255,8 @@ def qx_dequant(d: QxDesc, packed, out_kind: int, out, stream=None) -> None:
     import torch
     _chk_packed(d, packed)
     _chk(out, "out", torch.float16 if out_kind == QX_OUT_F16 else torch.uint8, d.n * d.k)
-    _check(load().qx_dequant(ctypes.byref(d), *_ptrs(packed), out_kind, *_ptrs(out), _stream(stream)),
-           "qx_dequant")
+    s = _here(stream, packed, out) if d.kind == QX_MX4 else _stream(stream)
+    _check(load().qx_dequant(ctypes.byref(d), *_ptrs(packed), out_kind, *_ptrs(out), s), "qx_dequant")
 
 
 def qx_gemv(d: QxDesc, packed, x, y, stream=None) -> None:
@@ -264,7 +264,8 @@ def qx_gemv(d: QxDesc, packed, x, y, stream=None) -> None:
     _chk_packed(d, packed)
     _chk(x, "x", torch.float16, d.k)
     _chk(y, "y", torch.float16, d.n)
-    _check(load().qx_gemv(ctypes.byref(d), *_ptrs(packed, x, y), _stream(stream)), "qx_gemv")
+    s = _here(stream, packed, x, y) if d.kind == QX_MX4 else _stream(stream)
+    _check(load().qx_gemv(ctypes.byref(d), *_ptrs(packed, x, y), s), "qx_gemv")
 
 
 def qx_gemv_a8(d: QxDesc, packed, x, y, stream=None) -> None:
@@ -282,8 +283,9 @@ def qx_gemm(d: QxDesc, packed, m: int, X, Y, stream=None) -> None:
     _rows(X, m, d.k, "X")
     _chk(X, "X", torch.float16, m * d.k)
     _chk(Y, "Y", torch.float16, m * d.n)
+    s = _here(stream, packed, X, Y) if d.kind == QX_MX4 else _stream(stream)
     p, x, y = _ptrs(packed, X, Y)
-    _check(load().qx_gemm(ctypes.byref(d), p, m, x, y, _stream(stream)), "qx_gemm")
+    _check(load().qx_gemm(ctypes.byref(d), p, m, x, y, s), "qx_gemm")
 
 
 def qx_quantize_a8(m: int, k: int, X, Xq, sx, stream=None) -> None:

@@ -12,7 +12,7 @@
 // a stage lie beside each other, 32 to 64 bytes a slice, which is what the loads cost most by: a stage of two
 // chunks takes 1.7 us of loads and 1.65 us of decoding and products without each other, 2.1 together (8 experts
 // of 1376x4096, uniform-4 g128, m = 999, 64 x 128: 27, 26.5 and 33.7 us). Measured: 30 us there (375 TFLOP/s),
-// 39 with the kernel of the single product; 32 experts, m = 64: 24 us, 90 MB of weights at 3.8 TB/s.
+// 39 with the kernel of the single product; 32 experts, m = 64: 24 us.
 #include "expert_tiles.h"
 #include "grouped_plan.h"
 #include "lds_loads.h"

@@ -73,6 +73,9 @@ int launch_gemv_seg(const qx_desc* d, const void* packed, const uint16_t* x, uin
 
 }  // namespace
 
+// As many waves a row as it has 2048 k, 8 at most. us with 1 / 2 / 4 / 8 waves a row, and in the tiles:
+// 22016x1024 5.0 / 5.5 / 7.1 / 9.3, 5.0; 22016x4096 9.8 / 9.3 / 10.2 / 11.7, 11.9 (5.2 TB/s); 4096x4096
+// 4.3 / 3.6 / 4.0 / 3.8, 4.8; 4096x8192 6.7 / 5.7 / 5.2 / 5.3, 7.0; 16384x11008 18.7 / 18.6 / 18.9 / 18.5, 26.1.
 int launch_gemv_mx4(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y, hipStream_t s) {
   if (d->k <= 2048) return launch_gemv_seg<1>(d, packed, x, y, s);
   if (d->k <= 4096) return launch_gemv_seg<2>(d, packed, x, y, s);

@@ -217,3 +217,41 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         qx._here(there, here, here)
     assert qx._here(here, here, here) == 7
     assert qx._here(None, here) == 5
+
+
+def test_products_of_more_tiles_than_a_launch_takes_are_refused():
+    """Before anything is enqueued: the sizes alone decide."""
+    lib = qx.load()
+    big = ctypes.byref(_desc(2**31 - 1, 128))
+    assert lib.qx_gemv(big, P(16), P(16), P(16), None) == qx.QX_E_UNSUPPORTED
+    assert lib.qx_gemm(big, P(16), 1, P(16), P(16), None) == qx.QX_E_UNSUPPORTED
+    for m in (2, 65536):
+        assert lib.qx_gemm(big, P(16), m, P(16), P(16), None) == qx.QX_E_UNSUPPORTED
+        assert lib.qx_gemm_a4(big, P(16), m, P(16), P(16), None) == qx.QX_E_UNSUPPORTED
+    for d in (_desc(2**31 - 1, 128), qx.desc(2**31 - 1, 128, 3, 64, qx.QX_CODEBOOK), qx.desc(2**31 - 1, 128, 4, 128, qx.QX_UNIFORM),
+              qx.desc(2**31 - 1, 128, 4, 64, qx.QX_Q4X)):
+        stride = qx.qx_blob_size(d) // 16 * 16 + 16
+        for m in (1, 300, 65536):
+            assert lib.qx_gemm_grouped(ctypes.byref(d), P(16), stride, 1024, m, P(16), P(16), P(16), None) == qx.QX_E_UNSUPPORTED
+    stride = qx.qx_blob_size(_desc(2**31 - 1, 128)) // 16 * 16 + 16
+    assert lib.qx_gemm_a4_grouped(big, P(16), stride, 1024, 65536, P(16), P(16), P(16), None) == qx.QX_E_UNSUPPORTED
+
+
+def test_mx4_calls_of_another_device_are_refused(monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+
+    class There(_Fake):
+        device = "cuda:1"
+
+        def get_device(self):
+            return 1
+
+    d = _desc(64, 256)
+    blob, x, X, Y = There(torch.uint8, qx.qx_blob_size(d)), There(torch.float16, 256), There(torch.float16, 4, 256), There(torch.float16, 64 * 256)
+    with pytest.raises(ValueError, match="current device"):
+        qx.qx_dequant(d, blob, qx.QX_OUT_F16, Y)
+    with pytest.raises(ValueError, match="current device"):
+        qx.qx_gemv(d, blob, x, Y)
+    with pytest.raises(ValueError, match="current device"):
+        qx.qx_gemm(d, blob, 4, X, Y)
