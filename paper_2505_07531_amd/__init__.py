@@ -324,6 +324,16 @@ def _here(stream, *tensors):
     return stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor for a call on `stream` to write, from that stream's own memory: what the current
+    stream freed it may still be writing."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def qx_quantize_mx4(m: int, k: int, X, packed, stream=None) -> None:
     import torch
     m, k = int(m), int(k)
@@ -390,7 +400,7 @@ def quantize_mx4(X, stream=None) -> "PackedWeight":
     """An fp16 device tensor [m][k], weights or activations, rounded to MX4 where it lies."""
     import torch
     m, k = X.shape
-    out = torch.empty(m * k // 32 * 17, dtype=torch.uint8, device=X.device)
+    out = _empty(m * k // 32 * 17, torch.uint8, X.device, stream)
     qx_quantize_mx4(m, k, X, out, stream)
     return PackedWeight._around(QxDesc(m, k, 4, 32, QX_MX4, 0), out, m * k // 32 * 17)
 
@@ -441,14 +451,14 @@ class PackedWeight:
     def dequant(self, out_kind: int = QX_OUT_F16, stream=None):
         import torch
         dt = torch.float16 if out_kind == QX_OUT_F16 else torch.uint8
-        out = torch.empty((self.desc.n, self.desc.k), dtype=dt, device=self.data.device)
+        out = _empty((self.desc.n, self.desc.k), dt, self.data.device, stream if self.desc.kind == QX_MX4 else None)
         qx_dequant(self.desc, self.data, out_kind, out, stream)
         return out
 
     def gemv(self, x, y=None, stream=None):
         import torch
         if y is None:
-            y = torch.empty(self.desc.n, dtype=torch.float16, device=x.device)
+            y = _empty(self.desc.n, torch.float16, x.device, stream if self.desc.kind == QX_MX4 else None)
         qx_gemv(self.desc, self.data, x, y, stream)
         return y
 
@@ -471,7 +481,7 @@ class PackedWeight:
         import torch
         m = X.shape[0]
         if Y is None:
-            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
+            Y = _empty((m, self.desc.n), torch.float16, X.device, stream if self.desc.kind == QX_MX4 else None)
         qx_gemm(self.desc, self.data, m, X, Y, stream)
         return Y
 
@@ -480,7 +490,7 @@ class PackedWeight:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
+            Y = _empty((m, self.desc.n), torch.float16, Xq.data.device, stream)
         qx_gemm_a4(self.desc, self.data, m, Xq.data, Y, stream)
         return Y
 
@@ -504,6 +514,8 @@ class PackedExperts:
     def stack(cls, weights) -> "PackedExperts":
         """From PackedWeights of one descriptor, copied side by side."""
         import torch
+        if not weights:
+            raise ValueError("no experts")
         d, size = weights[0].desc, weights[0].nbytes
         if any(bytes(w.desc) != bytes(d) for w in weights):
             raise ValueError("experts of different descriptors")
@@ -517,7 +529,7 @@ class PackedExperts:
         import torch
         m = X.shape[0]
         if Y is None:
-            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
+            Y = _empty((m, self.desc.n), torch.float16, X.device, stream)
         qx_gemm_grouped(self.desc, self.data, m, X, offsets, Y, stream)
         return Y
 
@@ -526,6 +538,6 @@ class PackedExperts:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
+            Y = _empty((m, self.desc.n), torch.float16, Xq.data.device, stream)
         qx_gemm_a4_grouped(self.desc, self.data, m, Xq.data, offsets, Y, stream)
         return Y

@@ -255,3 +255,12 @@ def test_mx4_calls_of_another_device_are_refused(monkeypatch):
         qx.qx_gemv(d, blob, x, Y)
     with pytest.raises(ValueError, match="current device"):
         qx.qx_gemm(d, blob, 4, X, Y)
+
+
+def test_a_stack_of_no_experts_or_of_different_ones_is_refused():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError):
+        qx.PackedExperts.stack([])
+    a, b = _desc(64, 256), _desc(32, 256)
+    with pytest.raises(ValueError):
+        qx.PackedExperts.stack([qx.PackedWeight.from_blob(d, _Fake(torch.uint8, qx.qx_blob_size(d))) for d in (a, b)])
