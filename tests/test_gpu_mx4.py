@@ -448,3 +448,18 @@ def test_codes_past_four_gigabytes(gpu):
         check(y[:, [0, n - 2, n - 1]], x[:m], w[[0, 0, 1]])
     y = pw.gemm_a4(gpu.quantize_mx4(to_dev(x))).cpu().numpy()
     check(y[:, [0, n - 2, n - 1]], mx4.levels(*mx4.quantize(x)), w[[0, 0, 1]])
+
+
+@pytest.mark.parametrize("m", [1, 2])
+@pytest.mark.parametrize("n,k", [(77, 2048), (1, 2176), (31, 4096), (4099, 4224), (33, 8320), (65, 16384), (9, 32768)])
+def test_one_and_two_rows(gpu, n, k, m):
+    """Long rows of weights, whole and in part of a wave's turn; a row of X that is NaN stays alone."""
+    q = random_mx4(n, k, n + k)
+    x = activations(k, 9, m)
+    pw = gpu.PackedWeight.from_quant(q)
+    w = mx4.dequant(q.codes, q.scales)
+    y = pw.gemm(to_dev(x)).cpu().numpy()
+    check(y, x, w)
+    x2 = np.concatenate([x[:1], np.full((1, k), np.nan, np.float16)])[:m]
+    again = pw.gemm(to_dev(x2)).cpu().numpy()
+    assert np.array_equal(again[:1].view(np.uint16), y[:1].view(np.uint16)) and np.isnan(again[1:]).all()
