@@ -324,12 +324,10 @@ def _here(stream, *tensors):
     return stream.cuda_stream
 
 
-def _empty(shape, dtype, device, stream):
+def _empty_on(stream, shape, dtype, device):
     """A new tensor for a call on `stream` to write, from that stream's own memory: what the current
     stream freed it may still be writing."""
     import torch
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
@@ -400,7 +398,10 @@ def quantize_mx4(X, stream=None) -> "PackedWeight":
     """An fp16 device tensor [m][k], weights or activations, rounded to MX4 where it lies."""
     import torch
     m, k = X.shape
-    out = _empty(m * k // 32 * 17, torch.uint8, X.device, stream)
+    if stream is None:
+        out = torch.empty(m * k // 32 * 17, dtype=torch.uint8, device=X.device)
+    else:
+        out = _empty_on(stream, m * k // 32 * 17, torch.uint8, X.device)
     qx_quantize_mx4(m, k, X, out, stream)
     return PackedWeight._around(QxDesc(m, k, 4, 32, QX_MX4, 0), out, m * k // 32 * 17)
 
@@ -451,14 +452,20 @@ class PackedWeight:
     def dequant(self, out_kind: int = QX_OUT_F16, stream=None):
         import torch
         dt = torch.float16 if out_kind == QX_OUT_F16 else torch.uint8
-        out = _empty((self.desc.n, self.desc.k), dt, self.data.device, stream if self.desc.kind == QX_MX4 else None)
+        if stream is None or self.desc.kind != QX_MX4:
+            out = torch.empty((self.desc.n, self.desc.k), dtype=dt, device=self.data.device)
+        else:
+            out = _empty_on(stream, (self.desc.n, self.desc.k), dt, self.data.device)
         qx_dequant(self.desc, self.data, out_kind, out, stream)
         return out
 
     def gemv(self, x, y=None, stream=None):
         import torch
         if y is None:
-            y = _empty(self.desc.n, torch.float16, x.device, stream if self.desc.kind == QX_MX4 else None)
+            if stream is None or self.desc.kind != QX_MX4:
+                y = torch.empty(self.desc.n, dtype=torch.float16, device=x.device)
+            else:
+                y = _empty_on(stream, self.desc.n, torch.float16, x.device)
         qx_gemv(self.desc, self.data, x, y, stream)
         return y
 
@@ -481,7 +488,10 @@ class PackedWeight:
         import torch
         m = X.shape[0]
         if Y is None:
-            Y = _empty((m, self.desc.n), torch.float16, X.device, stream if self.desc.kind == QX_MX4 else None)
+            if stream is None or self.desc.kind != QX_MX4:
+                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
+            else:
+                Y = _empty_on(stream, (m, self.desc.n), torch.float16, X.device)
         qx_gemm(self.desc, self.data, m, X, Y, stream)
         return Y
 
@@ -490,7 +500,10 @@ class PackedWeight:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            Y = _empty((m, self.desc.n), torch.float16, Xq.data.device, stream)
+            if stream is None:
+                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
+            else:
+                Y = _empty_on(stream, (m, self.desc.n), torch.float16, Xq.data.device)
         qx_gemm_a4(self.desc, self.data, m, Xq.data, Y, stream)
         return Y
 
@@ -529,7 +542,10 @@ class PackedExperts:
         import torch
         m = X.shape[0]
         if Y is None:
-            Y = _empty((m, self.desc.n), torch.float16, X.device, stream)
+            if stream is None:
+                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
+            else:
+                Y = _empty_on(stream, (m, self.desc.n), torch.float16, X.device)
         qx_gemm_grouped(self.desc, self.data, m, X, offsets, Y, stream)
         return Y
 
@@ -538,6 +554,9 @@ class PackedExperts:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            Y = _empty((m, self.desc.n), torch.float16, Xq.data.device, stream)
+            if stream is None:
+                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
+            else:
+                Y = _empty_on(stream, (m, self.desc.n), torch.float16, Xq.data.device)
         qx_gemm_a4_grouped(self.desc, self.data, m, Xq.data, offsets, Y, stream)
         return Y
