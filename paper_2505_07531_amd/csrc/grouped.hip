@@ -207,8 +207,19 @@ __global__ __launch_bounds__(THREADS, THREADS / 256) void grouped_kernel(const c
         l4[nt] = levels(buf, cc, 32 * g / G, wn * NT * 16 + nt * 16 + li, c);
       }
     }
+    // the rows of X are read a step ahead and stay there (64 x 128 tiles: 3 to 5 % less time than beside
+    // their products, where the compiler puts them)
+    h8_t x[2][MT];
+    auto read_x = [&](int T) {
+      const uint32_t xr = in_vgpr(S::kX + (wm * MT * 16 + li) * KU * 256 + ((cc * 16 + 4 * T + g) ^ li) * 16);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) x[T & 1][mt] = *reinterpret_cast<const h8_t*>(buf + (xr + mt * KU * 4096));
+    };
+    read_x(0);
 #pragma unroll
     for (int T = 0; T < 4; ++T) {
+      if (T < 3) read_x(T + 1);
+      __builtin_amdgcn_sched_barrier(0);
       h8_t w[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -231,13 +242,10 @@ __global__ __launch_bounds__(THREADS, THREADS / 256) void grouped_kernel(const c
           w[nt] = eight_weights<BITS, KIND>(q[0], q[1], levels(buf, cc, 32 * T / G, wn * NT * 16 + nt * 16 + li, c));
         }
       }
-      const uint32_t xr = in_vgpr(S::kX + (wm * MT * 16 + li) * KU * 256 + ((cc * 16 + 4 * T + g) ^ li) * 16);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const h8_t x = *reinterpret_cast<const h8_t*>(buf + (xr + mt * KU * 4096));
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[nt], x, acc[mt][nt], 0, 0, 0);
-      }
+        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[nt], x[T & 1][mt], acc[mt][nt], 0, 0, 0);
     }
   };
   auto compute = [&](int st, const char* buf) {
