@@ -29,6 +29,8 @@
 // (22016x4096, 8 rows: 13.2 to 20.7): two buffers.
 #pragma once
 
+#include <type_traits>
+
 #include "gemm_tile_plan.h"
 #include "lds_loads.h"
 #include "mx4_device.h"
@@ -166,8 +168,10 @@ struct Mx4Loads {
 template <class S>
 struct Mx4Unit {
   static constexpr int J = S::A4 ? 1 : 2;  // products of 32 k a unit
-  u32x4 q[J][S::NT], x[J][S::MT];          // MX4 pieces, or fp16 fragments
-  uint32_t qs[S::A4 ? S::NT : 1], xs[S::A4 ? S::MT : 1];
+  // MX4 rows: pieces of 32 codes. fp16 rows: 16 codes of a weight row, fragments of the rows
+  typename std::conditional<S::A4, u32x4, u32x2>::type q[S::NT];
+  u32x4 x[J][S::MT];
+  uint32_t qs[S::NT], xs[S::A4 ? S::MT : 1];  // scales in the low byte
 
   // Unit u of the buffer; its scales are in the dword at `sd` of a row's 16 bytes in `sbuf`, from byte
   // `sb` of it on.
@@ -182,7 +186,7 @@ struct Mx4Unit {
       const int xr = (int)in_vgpr(S::kW + (wm * S::MT * 16 + li) * S::XP * 16 + ((u * 4 + g) ^ sx) * 16);
 #pragma unroll
       for (int nt = 0; nt < S::NT; ++nt) {
-        q[0][nt] = *reinterpret_cast<const u32x4*>(buf + (wr + nt * 256 * S::WP));
+        q[nt] = *reinterpret_cast<const u32x4*>(buf + (wr + nt * 256 * S::WP));
         qs[nt] = *reinterpret_cast<const uint32_t*>(sbuf + (sw4 + nt * 256)) >> (8 * g);
       }
 #pragma unroll
@@ -196,11 +200,8 @@ struct Mx4Unit {
       const int xr1 = (int)in_vgpr(S::kW + (wm * S::MT * 16 + li) * S::XP * 16 + ((u * 8 + 4 + g) ^ sx) * 16);
 #pragma unroll
       for (int nt = 0; nt < S::NT; ++nt) {
-        const u32x2 d = *reinterpret_cast<const u32x2*>(buf + (wr + nt * 256 * S::WP));
-        const uint32_t sv = *reinterpret_cast<const uint32_t*>(sbuf + (sw4 + nt * 256));
-        const float scale = __builtin_bit_cast(float, ((sv >> (8 * sb + 8 * (g >> 1))) & 255u) << 23);
-        q[0][nt] = __builtin_bit_cast(u32x4, mx4_frag(d.x, scale));
-        q[1][nt] = __builtin_bit_cast(u32x4, mx4_frag(d.y, scale));
+        q[nt] = *reinterpret_cast<const u32x2*>(buf + (wr + nt * 256 * S::WP));
+        qs[nt] = *reinterpret_cast<const uint32_t*>(sbuf + (sw4 + nt * 256)) >> (8 * sb + 8 * (g >> 1));
       }
 #pragma unroll
       for (int mt = 0; mt < S::MT; ++mt) {
@@ -211,18 +212,27 @@ struct Mx4Unit {
   }
 
   __device__ __forceinline__ void multiply(f4_t (&acc)[S::MT][S::NT]) const {
+    // All reads before the first product, not each beside its own as the compiler would: MX4 rows 22016x4096,
+    // m = 4096 237 us, 248 without; fp16 rows, 32 experts of 2816x4096, m = 8192 in 64 x 128 232, 245. The
+    // 128 x 64 wave tile has no registers for it with fp16 rows (22016x4096, m = 4096 546, 795 with it).
+    if constexpr (S::A4 || S::MT < 8) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j) {
+      h8_t w[S::A4 ? 1 : S::NT];
+      if constexpr (!S::A4)
+#pragma unroll
+        for (int nt = 0; nt < S::NT; ++nt)
+          w[nt] = mx4_frag(q[nt][j], __builtin_bit_cast(float, (qs[nt] & 255u) << 23));
 #pragma unroll
       for (int mt = 0; mt < S::MT; ++mt)
 #pragma unroll
         for (int nt = 0; nt < S::NT; ++nt) {
           if constexpr (S::A4)
-            acc[mt][nt] = mfma_mx4(q[0][nt], qs[nt], x[0][mt], xs[mt], acc[mt][nt]);
+            acc[mt][nt] = mfma_mx4(q[nt], qs[nt], x[0][mt], xs[mt], acc[mt][nt]);
           else
-            acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, q[j][nt]),
-                                                                 __builtin_bit_cast(h8_t, x[j][mt]), acc[mt][nt], 0, 0, 0);
+            acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[nt], __builtin_bit_cast(h8_t, x[j][mt]), acc[mt][nt], 0, 0, 0);
         }
+    }
   }
 };
 
