@@ -10,8 +10,8 @@
 // tables and rows go straight to LDS a stage ahead, one barrier a stage, and k is split over the waves of a
 // block, whose sums are added in their order. A piece of codes is 16 bytes of a chunk and slice; the chunks of
 // a stage lie beside each other, 32 to 64 bytes a slice, which is what the loads cost most by: a stage of two
-// chunks takes 1.7 us of loads and 1.65 us of decoding and products without each other, 2.1 together (8 experts
-// of 1376x4096, uniform-4 g128, m = 999, 64 x 128: 27, 26.5 and 33.7 us). Measured: 30 us there (375 TFLOP/s),
+// chunks takes 1.7 us of loads and 1.65 us of decoding and products without each other, 2.0 together (8 experts
+// of 1376x4096, uniform-4 g128, m = 999, 64 x 128: 27, 26.5 and 31.6 us). Measured: 28 us there (400 TFLOP/s),
 // 39 with the kernel of the single product; 32 experts, m = 64: 24 us.
 #include "expert_tiles.h"
 #include "grouped_plan.h"

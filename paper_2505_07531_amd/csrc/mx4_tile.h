@@ -19,8 +19,8 @@
 // order of the waves. The outputs of large tiles pass through LDS, so that stores write whole rows of
 // the tile (32-byte pieces: 9 us more of 183). The order of the sums is fixed: the same bits every time.
 //
-// Measured (us, and TFLOP/s): MX4 rows 22016x4096, m = 4096: 238 (3100; 218 to 250 by the card's clock); fp16
-// rows 11008x4096, m = 2001: 174 (1040), where a library product of fp16 matrices of 8192^3 reaches 1140; 32
+// Measured (us, and TFLOP/s): MX4 rows 22016x4096, m = 4096: 228 (3240); fp16
+// rows 11008x4096, m = 2001: 170 (1060), where a library product of fp16 matrices of 8192^3 reaches 1140; 32
 // experts of 2816x4096, 32 fp16 rows: 20.8 (5.0 TB/s). The largest tiles' time is a third products, the
 // rest the start and end of a tile (all compute units store at once) and loads. Deeper rings of smaller
 // stages there, and halves of a block's waves multiplying and loading in turn, were not faster (285 to 320 us
