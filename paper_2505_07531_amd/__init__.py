@@ -24,9 +24,8 @@ Functions keep the C names:
 Tensor arguments are torch CUDA tensors (HIP device memory); ``stream`` is a
 torch stream (default: the current stream). Before a device call the binding
 checks each tensor against the descriptor (device, dtype, contiguity, element
-count) and raises ValueError without launching anything when one does not fit.
-The calls of the microscaled and grouped products also check that every tensor
-lies on the current device, where they launch.
+count) and raises ValueError without launching anything when one does not fit,
+or does not lie on the current device, where the call launches.
 """
 from __future__ import annotations
 
@@ -241,74 +240,6 @@ def _rows(X, m: int, k: int, name: str):
         raise ValueError(f"{name}: shape {tuple(X.shape)}, expected ({m}, {k})")
 
 
-def _stream(stream):
-    if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # no Stream object
-        if raw is not None:
-            return raw(torch._C._cuda_getDevice())
-        stream = torch.cuda.current_stream()
-    return stream.cuda_stream
-
-
-def qx_dequant(d: QxDesc, packed, out_kind: int, out, stream=None) -> None:
-    import torch
-    _chk_packed(d, packed)
-    _chk(out, "out", torch.float16 if out_kind == QX_OUT_F16 else torch.uint8, d.n * d.k)
-    s = _here(stream, packed, out) if d.kind == QX_MX4 else _stream(stream)
-    _check(load().qx_dequant(ctypes.byref(d), *_ptrs(packed), out_kind, *_ptrs(out), s), "qx_dequant")
-
-
-def qx_gemv(d: QxDesc, packed, x, y, stream=None) -> None:
-    import torch
-    _chk_packed(d, packed)
-    _chk(x, "x", torch.float16, d.k)
-    _chk(y, "y", torch.float16, d.n)
-    s = _here(stream, packed, x, y) if d.kind == QX_MX4 else _stream(stream)
-    _check(load().qx_gemv(ctypes.byref(d), *_ptrs(packed, x, y), s), "qx_gemv")
-
-
-def qx_gemv_a8(d: QxDesc, packed, x, y, stream=None) -> None:
-    import torch
-    _chk_packed(d, packed)
-    _chk(x, "x", torch.float16, d.k)
-    _chk(y, "y", torch.float16, d.n)
-    _check(load().qx_gemv_a8(ctypes.byref(d), *_ptrs(packed, x, y), _stream(stream)), "qx_gemv_a8")
-
-
-def qx_gemm(d: QxDesc, packed, m: int, X, Y, stream=None) -> None:
-    import torch
-    m = int(m)
-    _chk_packed(d, packed)
-    _rows(X, m, d.k, "X")
-    _chk(X, "X", torch.float16, m * d.k)
-    _chk(Y, "Y", torch.float16, m * d.n)
-    s = _here(stream, packed, X, Y) if d.kind == QX_MX4 else _stream(stream)
-    p, x, y = _ptrs(packed, X, Y)
-    _check(load().qx_gemm(ctypes.byref(d), p, m, x, y, s), "qx_gemm")
-
-
-def qx_quantize_a8(m: int, k: int, X, Xq, sx, stream=None) -> None:
-    import torch
-    m, k = int(m), int(k)
-    _chk(X, "X", torch.float16, m * k)
-    _chk(Xq, "Xq", torch.int8, m * k)
-    _chk(sx, "sx", torch.float32, m)
-    _check(load().qx_quantize_a8(m, k, *_ptrs(X, Xq, sx), _stream(stream)), "qx_quantize_a8")
-
-
-def qx_gemm_a8(d: QxDesc, packed, m: int, Xq, sx, Y, stream=None) -> None:
-    import torch
-    m = int(m)
-    _chk_packed(d, packed)
-    _rows(Xq, m, d.k, "Xq")
-    _chk(Xq, "Xq", torch.int8, m * d.k)
-    _chk(sx, "sx", torch.float32, m)
-    _chk(Y, "Y", torch.float16, m * d.n)
-    p, xq, s_, y = _ptrs(packed, Xq, sx, Y)
-    _check(load().qx_gemm_a8(ctypes.byref(d), p, m, xq, s_, y, _stream(stream)), "qx_gemm_a8")
-
-
 def _here(stream, *tensors):
     """The raw stream, once every tensor is known to lie on the current device (a launch goes to
     the current device, whatever the tensors' own)."""
@@ -318,7 +249,7 @@ def _here(stream, *tensors):
         if t.get_device() != at:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{at}")
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(at)
+        return torch._C._cuda_getCurrentRawStream(at)  # no Stream object
     if stream.device.index != at:
         raise ValueError(f"stream of {stream.device}, but the current device is cuda:{at}")
     return stream.cuda_stream
@@ -330,6 +261,67 @@ def _empty_on(stream, shape, dtype, device):
     import torch
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def qx_dequant(d: QxDesc, packed, out_kind: int, out, stream=None) -> None:
+    import torch
+    _chk_packed(d, packed)
+    _chk(out, "out", torch.float16 if out_kind == QX_OUT_F16 else torch.uint8, d.n * d.k)
+    s = _here(stream, packed, out)
+    _check(load().qx_dequant(ctypes.byref(d), *_ptrs(packed), out_kind, *_ptrs(out), s), "qx_dequant")
+
+
+def qx_gemv(d: QxDesc, packed, x, y, stream=None) -> None:
+    import torch
+    _chk_packed(d, packed)
+    _chk(x, "x", torch.float16, d.k)
+    _chk(y, "y", torch.float16, d.n)
+    s = _here(stream, packed, x, y)
+    _check(load().qx_gemv(ctypes.byref(d), *_ptrs(packed, x, y), s), "qx_gemv")
+
+
+def qx_gemv_a8(d: QxDesc, packed, x, y, stream=None) -> None:
+    import torch
+    _chk_packed(d, packed)
+    _chk(x, "x", torch.float16, d.k)
+    _chk(y, "y", torch.float16, d.n)
+    s = _here(stream, packed, x, y)
+    _check(load().qx_gemv_a8(ctypes.byref(d), *_ptrs(packed, x, y), s), "qx_gemv_a8")
+
+
+def qx_gemm(d: QxDesc, packed, m: int, X, Y, stream=None) -> None:
+    import torch
+    m = int(m)
+    _chk_packed(d, packed)
+    _rows(X, m, d.k, "X")
+    _chk(X, "X", torch.float16, m * d.k)
+    _chk(Y, "Y", torch.float16, m * d.n)
+    s = _here(stream, packed, X, Y)
+    p, x, y = _ptrs(packed, X, Y)
+    _check(load().qx_gemm(ctypes.byref(d), p, m, x, y, s), "qx_gemm")
+
+
+def qx_quantize_a8(m: int, k: int, X, Xq, sx, stream=None) -> None:
+    import torch
+    m, k = int(m), int(k)
+    _chk(X, "X", torch.float16, m * k)
+    _chk(Xq, "Xq", torch.int8, m * k)
+    _chk(sx, "sx", torch.float32, m)
+    s = _here(stream, X, Xq, sx)
+    _check(load().qx_quantize_a8(m, k, *_ptrs(X, Xq, sx), s), "qx_quantize_a8")
+
+
+def qx_gemm_a8(d: QxDesc, packed, m: int, Xq, sx, Y, stream=None) -> None:
+    import torch
+    m = int(m)
+    _chk_packed(d, packed)
+    _rows(Xq, m, d.k, "Xq")
+    _chk(Xq, "Xq", torch.int8, m * d.k)
+    _chk(sx, "sx", torch.float32, m)
+    _chk(Y, "Y", torch.float16, m * d.n)
+    s = _here(stream, packed, Xq, sx, Y)
+    p, xq, s_, y = _ptrs(packed, Xq, sx, Y)
+    _check(load().qx_gemm_a8(ctypes.byref(d), p, m, xq, s_, y, s), "qx_gemm_a8")
 
 
 def qx_quantize_mx4(m: int, k: int, X, packed, stream=None) -> None:
