@@ -255,10 +255,12 @@ def _here(stream, *tensors):
     return stream.cuda_stream
 
 
-def _empty_on(stream, shape, dtype, device):
-    """A new tensor for a call on `stream` to write, from that stream's own memory: what the current
-    stream freed it may still be writing."""
+def _new(stream, shape, dtype, device):
+    """A new tensor for a call to write; for one on a given stream from that stream's own memory,
+    since what the current stream freed it may still be writing."""
     import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
@@ -390,10 +392,7 @@ def quantize_mx4(X, stream=None) -> "PackedWeight":
     """An fp16 device tensor [m][k], weights or activations, rounded to MX4 where it lies."""
     import torch
     m, k = X.shape
-    if stream is None:
-        out = torch.empty(m * k // 32 * 17, dtype=torch.uint8, device=X.device)
-    else:
-        out = _empty_on(stream, m * k // 32 * 17, torch.uint8, X.device)
+    out = _new(stream, m * k // 32 * 17, torch.uint8, X.device)
     qx_quantize_mx4(m, k, X, out, stream)
     return PackedWeight._around(QxDesc(m, k, 4, 32, QX_MX4, 0), out, m * k // 32 * 17)
 
@@ -402,8 +401,8 @@ def quantize_a8(X, stream=None):
     """(Xq int8 [m][k], sx fp32 [m]) of an fp16 [m][k] device tensor."""
     import torch
     m, k = X.shape
-    Xq = torch.empty((m, k), dtype=torch.int8, device=X.device)
-    sx = torch.empty(m, dtype=torch.float32, device=X.device)
+    Xq = _new(stream, (m, k), torch.int8, X.device)
+    sx = _new(stream, m, torch.float32, X.device)
     qx_quantize_a8(m, k, X, Xq, sx, stream)
     return Xq, sx
 
@@ -444,20 +443,14 @@ class PackedWeight:
     def dequant(self, out_kind: int = QX_OUT_F16, stream=None):
         import torch
         dt = torch.float16 if out_kind == QX_OUT_F16 else torch.uint8
-        if stream is None or self.desc.kind != QX_MX4:
-            out = torch.empty((self.desc.n, self.desc.k), dtype=dt, device=self.data.device)
-        else:
-            out = _empty_on(stream, (self.desc.n, self.desc.k), dt, self.data.device)
+        out = _new(stream, (self.desc.n, self.desc.k), dt, self.data.device)
         qx_dequant(self.desc, self.data, out_kind, out, stream)
         return out
 
     def gemv(self, x, y=None, stream=None):
         import torch
         if y is None:
-            if stream is None or self.desc.kind != QX_MX4:
-                y = torch.empty(self.desc.n, dtype=torch.float16, device=x.device)
-            else:
-                y = _empty_on(stream, self.desc.n, torch.float16, x.device)
+            y = _new(stream, self.desc.n, torch.float16, x.device)
         qx_gemv(self.desc, self.data, x, y, stream)
         return y
 
@@ -465,14 +458,14 @@ class PackedWeight:
         import torch
         m = Xq.shape[0]
         if Y is None:
-            Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.device)
+            Y = _new(stream, (m, self.desc.n), torch.float16, Xq.device)
         qx_gemm_a8(self.desc, self.data, m, Xq, sx, Y, stream)
         return Y
 
     def gemv_a8(self, x, y=None, stream=None):
         import torch
         if y is None:
-            y = torch.empty(self.desc.n, dtype=torch.float16, device=x.device)
+            y = _new(stream, self.desc.n, torch.float16, x.device)
         qx_gemv_a8(self.desc, self.data, x, y, stream)
         return y
 
@@ -480,10 +473,7 @@ class PackedWeight:
         import torch
         m = X.shape[0]
         if Y is None:
-            if stream is None or self.desc.kind != QX_MX4:
-                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
-            else:
-                Y = _empty_on(stream, (m, self.desc.n), torch.float16, X.device)
+            Y = _new(stream, (m, self.desc.n), torch.float16, X.device)
         qx_gemm(self.desc, self.data, m, X, Y, stream)
         return Y
 
@@ -492,10 +482,7 @@ class PackedWeight:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            if stream is None:
-                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
-            else:
-                Y = _empty_on(stream, (m, self.desc.n), torch.float16, Xq.data.device)
+            Y = _new(stream, (m, self.desc.n), torch.float16, Xq.data.device)
         qx_gemm_a4(self.desc, self.data, m, Xq.data, Y, stream)
         return Y
 
@@ -534,10 +521,7 @@ class PackedExperts:
         import torch
         m = X.shape[0]
         if Y is None:
-            if stream is None:
-                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=X.device)
-            else:
-                Y = _empty_on(stream, (m, self.desc.n), torch.float16, X.device)
+            Y = _new(stream, (m, self.desc.n), torch.float16, X.device)
         qx_gemm_grouped(self.desc, self.data, m, X, offsets, Y, stream)
         return Y
 
@@ -546,9 +530,6 @@ class PackedExperts:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            if stream is None:
-                Y = torch.empty((m, self.desc.n), dtype=torch.float16, device=Xq.data.device)
-            else:
-                Y = _empty_on(stream, (m, self.desc.n), torch.float16, Xq.data.device)
+            Y = _new(stream, (m, self.desc.n), torch.float16, Xq.data.device)
         qx_gemm_a4_grouped(self.desc, self.data, m, Xq.data, offsets, Y, stream)
         return Y

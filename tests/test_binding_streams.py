@@ -1,5 +1,5 @@
 """Devices and streams of the binding's calls, of every kind, without a GPU: tensors of another device are
-refused before a launch."""
+refused before a launch, and the outputs of a call on a given stream are allocated on that stream."""
 import contextlib
 from types import SimpleNamespace
 
@@ -102,3 +102,15 @@ def test_a_stream_of_another_device_is_refused(monkeypatch, name, kind, call):
     Allocations(monkeypatch, current=1)
     with pytest.raises(ValueError, match="current device"):
         call(SimpleNamespace(device=SimpleNamespace(index=0), cuda_stream=3))
+
+
+@pytest.mark.parametrize("name,kind,call", CALLS, ids=IDS)
+def test_outputs_are_allocated_on_the_stream_that_writes_them(monkeypatch, name, kind, call):
+    """What the current stream freed it may still be writing."""
+    made = Allocations(monkeypatch, current=1)
+    given = SimpleNamespace(device=SimpleNamespace(index=1), cuda_stream=3)
+    for stream in (given, None):
+        made.on.clear()
+        with pytest.raises(AssertionError, match="pointer"):  # all checks passed
+            call(stream)
+        assert made.on == [stream] * (2 if name == "quantize_a8" else 1)
