@@ -119,14 +119,16 @@ __global__ __launch_bounds__(THREADS, THREADS / 256) void grouped_kernel(const c
     const int cc = (q % KU) ^ (row * KU / 16 & (KU - 1));  // 16 rows of a chunk lie in 16 different places mod 256 bytes
     wat[i] = ((min(row, wlast) * BITS + s) * C + min(cc, C - 1)) * 16;
   }
+  // where a format has none of them the loop runs no turn, but is compiled: divisors of 1 then
+  constexpr int kParts = S::kParts + !S::kParts, kWords = S::kWords + !S::kWords;
 #pragma unroll
   for (int i = 0; i < S::loads(S::kTPieces); ++i) {
-    const int q = i * NTH + t, row = q % BN, part = q / BN % S::kParts, cc = min(q / (BN * S::kParts), KU - 1);
-    tat[i] = (min(row, wlast) * C + min(cc, C - 1)) * S::kParts * 16 + part * 16;
+    const int q = i * NTH + t, row = q % BN, part = q / BN % kParts, cc = min(q / (BN * kParts), KU - 1);
+    tat[i] = (min(row, wlast) * C + min(cc, C - 1)) * kParts * 16 + part * 16;
   }
 #pragma unroll
   for (int i = 0; i < S::loads(S::kMWords); ++i) {
-    const int q = i * NTH + t, row = q % BN, w = q / BN % (S::kWords + !S::kWords), cc = min(min(q / (BN * (S::kWords + !S::kWords)), KU - 1), C - 1);
+    const int q = i * NTH + t, row = q % BN, w = q / BN % kWords, cc = min(min(q / (BN * kWords), KU - 1), C - 1);
     if (KIND == QX_UNIFORM) mat[i] = (min(row, wlast) * G_row + cc * NG + w) * 4;
     else mat[i] = w == 0 ? (min(row, wlast) * G_row + cc * 2) * 2 : min(row, wlast) * words * 4;  // selectors: of the row
   }
