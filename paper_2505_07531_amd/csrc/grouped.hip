@@ -255,15 +255,15 @@ __global__ __launch_bounds__(THREADS, THREADS / 256) void grouped_kernel(const c
     if (c < C) chunk(buf, c - first(st), c);
   };
   load(0, lds0);
-  __syncthreads();
+  lds_loaded();
   int st = 0;
   for (; st + 1 < stages; st += 2) {
     load(st + 1, lds1);
     compute(st, lds0);
-    __syncthreads();
+    lds_loaded();
     if (st + 2 < stages) load(st + 2, lds0);
     compute(st + 1, lds1);
-    __syncthreads();
+    lds_loaded();
   }
   if (st < stages) compute(st, lds0);
 

@@ -18,6 +18,14 @@ __device__ __forceinline__ void load_lds(const char* src, char* dst) {
     __builtin_amdgcn_global_load_lds((GlobalVoid*)src, (LdsVoid*)dst, 4, 0, 0);
 }
 
+// Between loads to LDS and their reads by any wave of the block: a wave waits for its own loads, which the
+// barrier alone does not (they count as loads from memory, and __syncthreads orders LDS), then for the
+// other waves. The wait is vmcnt(0) with the other counters at their maximum.
+__device__ __forceinline__ void lds_loaded() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+}
+
 // Neighbouring columns of a row of Y, which may start at any multiple of 2 bytes.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));

@@ -339,15 +339,15 @@ __global__ __launch_bounds__(S::kThreads, (S::kWaves + 3) / 4) void mx4_tile_ker
   };
   ld.load(0, lds0);
   ld.load_scales(0, scales);
-  __syncthreads();
+  lds_loaded();
   int st = 0;
   for (; st + 1 < stages; st += 2) {
     ld.load(st + 1, lds1);
     compute(st, lds0);
-    __syncthreads();
+    lds_loaded();
     if (st + 2 < stages) ld.load(st + 2, lds0);
     compute(st + 1, lds1);
-    __syncthreads();
+    lds_loaded();
   }
   if (st < stages) compute(st, lds0);
 
