@@ -115,3 +115,57 @@ def test_grouped_shapes(gpu, bits, kind, group, shape, n, k, m):
     x, off = fp16_rows(m, k, 4), split_of(m, 8, n + m)
     same_grouped(run_grouped(gpu, pe, x, off), x, ws, off)
 
+
+# ------------------------------------------------------------------ long rows
+LONG = [(31, 4224), (77, 8320), (19, 11008), (65, 16384), (9, 32768)]
+
+
+@pytest.mark.parametrize("n,k", LONG)
+@pytest.mark.parametrize("m", [1, 2, 3, 9, 40, 200])
+def test_mx4_long_rows(gpu, n, k, m):
+    codes, scales = mx4_weights(n, k, n)
+    w, x = mx4.levels(codes, scales), fp16_rows(m, k, m)
+    pw = packed(gpu, codes, scales)
+    same(pw.gemm(to_dev(x)).cpu().numpy(), exact(x, w))
+    if m == 1:
+        same(pw.gemv(to_dev(x[0])).cpu().numpy(), exact(x, w)[0])
+    xc, xs = mx4_weights(m, k, m, 127, 127)
+    same(pw.gemm_a4(rows_of(gpu, xc, xs)).cpu().numpy(), exact(mx4.levels(xc, xs), w))
+
+
+@pytest.mark.parametrize("n,k", [(31, 4224), (19, 11008), (9, 32768)])
+@pytest.mark.parametrize("m", [1, 2, 3, 9, 40, 200])
+def test_mx4_one_block_of_a_long_row(gpu, n, k, m):
+    """Rows of X that are zero but for one block, the first and last of them and some between: nothing of
+    that block is lost among other terms, and W' of any scale of fp16's range."""
+    rng = np.random.default_rng(m)
+    codes, scales = mx4_weights(n, k, n, 112, 130)
+    pw = packed(gpu, codes, scales)
+    w = mx4.dequant(codes, scales)
+    at = np.concatenate([[k // 32 - 1, 0, k // 32 - 2], rng.integers(0, k // 32, m)])[:m] * 32 + rng.integers(0, 32, m)
+    x = np.zeros((m, k), np.float16)
+    x[np.arange(m), at] = rng.choice([-1.0, 1.0, 2.0], m)
+    want = (w[:, at].T * x[np.arange(m), at][:, None]).astype(np.float16)
+    same(pw.gemm(to_dev(x)).cpu().numpy(), want)
+    same(pw.gemm_a4(gpu.quantize_mx4(to_dev(x))).cpu().numpy(), want)
+    if m == 1:
+        same(pw.gemv(to_dev(x[0])).cpu().numpy(), want[0])
+
+
+@pytest.mark.parametrize("bits,kind,group", FORMATS)
+@pytest.mark.parametrize("n,k,m", [(19, 11008, 5), (33, 16384, 40)])
+def test_grouped_long_rows(gpu, bits, kind, group, n, k, m):
+    both = [small_weights(gpu, bits, kind, group, n, k, 40 + e) for e in range(3)]
+    pe, ws = gpu.PackedExperts.stack([w for w, _ in both]), [w for _, w in both]
+    x, off = fp16_rows(m, k, 4, 2), split_of(m, 3, 1)
+    same_grouped(run_grouped(gpu, pe, x, off), x, ws, off)
+
+
+@pytest.mark.parametrize("a4", [False, True])
+@pytest.mark.parametrize("n,k,m", [(19, 11008, 5), (33, 16384, 40), (65, 8320, 300)])
+def test_mx4_grouped_long_rows(gpu, a4, n, k, m):
+    cs = [mx4_weights(n, k, 50 + e) for e in range(3)]
+    pe, ws, off = gpu.PackedExperts.stack([packed(gpu, *c) for c in cs]), [mx4.levels(*c) for c in cs], split_of(m, 3, 1)
+    x = fp16_rows(m, k, 6, 2)  # 0, 1 and 2: the same in MX4
+    x[:, ::32] = 2             # a block's scale is that of its largest
+    same_grouped(run_grouped(gpu, pe, x, off, a4=a4), x, ws, off)
