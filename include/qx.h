@@ -311,8 +311,9 @@ int qx_gemm_a4(const qx_desc* d, const void* packed, int32_t m, const void* Xq, 
  *            are held to [0, m] and an expert that ends before it begins has no
  *            rows; which rows are written for offsets that decrease is not
  *            specified, but never any outside of Y.
- * Products, sums and rounding as qx_gemm's on the matrix cores. m = 0, n = 0 or
- * no experts is a no-op; m must be <= 65536. QX_E_UNSUPPORTED when the tiles of
+ * Products, sums and rounding as qx_gemm's on the matrix cores: of W' as
+ * qx_dequant writes it, also for an expert of a single row (qx_gemv takes the
+ * exact levels of uniform weights there). m = 0, n = 0 or no experts is a no-op; m must be <= 65536. QX_E_UNSUPPORTED when the tiles of
  * m rows by n columns are more than one launch takes (4194304 blocks).
  * Deterministic.
  */

@@ -6,13 +6,19 @@
 // registers in the order of k, 8 a lane, so that rows of X go to LDS as they are; the products are
 // v_mfma_f32_16x16x32_f16 with fp32 sums, weights first: a lane ends with four columns of Y.
 //
+// The rounding of uniform levels to fp16 is that of W' itself, as on the matrix cores of qx_gemm. Y is then as
+// far from 64-bit products of W' as its own rounding takes it (2.07e-4 in the norm, uniform-4 g128, k = 4096),
+// and 2.68e-4 from products of the unrounded levels. To multiply with q - z and scale the sums of every group
+// instead would take four multiply-adds a lane and tile of 16 x 16 for each group, at g32 beside every single
+// product instruction.
+//
 // Experts have few rows each, so a tile is small and its time is that of one block's chain over k: codes,
 // tables and rows go straight to LDS a stage ahead, one barrier a stage, and k is split over the waves of a
 // block, whose sums are added in their order. A piece of codes is 16 bytes of a chunk and slice; the chunks of
-// a stage lie beside each other, 32 to 64 bytes a slice, which is what the loads cost most by: a stage of two
-// chunks takes 1.7 us of loads and 1.65 us of decoding and products without each other, 2.0 together (8 experts
-// of 1376x4096, uniform-4 g128, m = 999, 64 x 128: 27, 26.5 and 31.6 us). Measured: 28 us there (400 TFLOP/s),
-// 39 with the kernel of the single product; 32 experts, m = 64: 24 us.
+// a stage lie beside each other, 32 to 64 bytes a slice, which is what the loads cost most by: 8 experts of
+// 1376x4096, uniform-4 g128, m = 999, in 64 x 128 take 28.3 us (398 TFLOP/s), the loads alone 27.3, decoding and
+// products alone 21.6 (blobs in the last-level cache; read from memory 31.1, 29.2 and 21.6). 32 experts of that
+// size, m = 64, from memory: 25 us.
 #include "expert_tiles.h"
 #include "grouped_plan.h"
 #include "lds_loads.h"

@@ -9,13 +9,15 @@ namespace grouped {
 
 // The last shape is C of gemm_tile.hip (128 x 192), the others are those of grouped.hip, ks chunks a stage.
 // Costs as in mx4_plan.h, fitted to the times of 181 sizes (4 to 128 experts, n = 256 to 6000, k = 512 to 5120,
-// 1 to 300 rows each, unevenly shared, weights read from memory): of uniform-4 g128, uniform-3 g64 and
-// codebook-3 g128, and of codebook-4 g64, whose table reads fill LDS. Where a shape is within 30 % of the
-// best, 96 of 100 are within 25 %; the shapes that they choose take 3.9 and 2.4 % more than the best in the
-// mean. us in the order of the list, uniform-4 g128: 8 experts of 576x3584, m = 108 8.0 / 12.0 / 13.2 / 24 / 28;
-// 66 of 694x1024, m = 940 17 / 13 / 16 / 22 / 18; 5 of 916x3840, m = 361 (from the third on) 15 / 26 / 30 / 62; 7 of
-// 2057x2688, m = 402 29 / 25 / 24 / 22 / 25 / 47; 78 of 3398x768, m = 3471 205 / 107 / 83 / 104 / 65 / 87; 5 of
-// 5205x3712, m = 808 (from the third on) 92 / 95 / 94 / 70.
+// 1 to 300 rows each, unevenly shared): of uniform-4 g128, uniform-3 g64 and codebook-3 g128, and of codebook-4
+// g64, whose table reads fill LDS; before the rows of X were read a step ahead. With the present kernels and
+// 1.2 GB of weights read in turn the shapes that they choose take 2.4 to 3.7 % more than the best of all in the
+// mean, in each of the 13 formats (uniform-4 g64 the most, codebook-4 g64 the least, Q4X 3.5; at most 53 %); where
+// a shape is within 30 % of the best, 96 of 100 costs are within 23 to 32 % of its time, 40 % with codebooks of
+// groups of 32. us in the order of the list, uniform-4 g128: 8 experts of 576x3584, m = 108 9.3 / 14.5 / 15.6 /
+// 26 / 31 / 61; 66 of 694x1024, m = 940 18.5 / 14.8 / 17.6 / 23 / 18.3 / 33; 5 of 916x3840, m = 361 18.1 / 19.6 /
+// 17.2 / 28 / 33 / 66; 7 of 2057x2688, m = 402 30 / 28 / 26 / 25 / 27 / 50; 78 of 3398x768, m = 3471 204 / 107 /
+// 85 / 103 / 65 / 87; 5 of 5205x3712, m = 808 139 / 130 / 94 / 93 / 96 / 70.
 constexpr int kShapes = 6, kTile = 5;
 using mx4::ShapeCost;
 inline constexpr ShapeCost shapes[2][kShapes] = {

@@ -90,15 +90,16 @@ int launch_gemv_rows(const qx_desc* d, const void* packed, const uint16_t* x, ui
 }  // namespace
 
 // As many waves a row as it has 2048 k, 8 at most. us with 1 / 2 / 4 / 8 waves a row, and in the tiles:
-// 22016x1024 5.0 / 5.5 / 7.1 / 9.3, 5.0; 22016x4096 9.8 / 9.3 / 10.2 / 11.7, 11.9 (5.2 TB/s); 4096x4096
-// 4.3 / 3.6 / 4.0 / 3.8, 4.8; 4096x8192 6.7 / 5.7 / 5.2 / 5.3, 7.0; 16384x11008 18.7 / 18.6 / 18.9 / 18.5, 26.1.
+// 22016x1024 4.9 / 5.4 / 7.0 / 9.2, 5.3; 22016x4096 9.8 / 9.4 / 10.1 / 11.6, 11.9 (5.1 TB/s); 4096x4096
+// 4.3 / 3.6 / 4.0 / 3.8, 5.8; 4096x8192 6.7 / 5.9 / 5.2 / 5.3, 8.8; 16384x11008 18.7 / 18.1 / 18.7 / 18.4, 25.7
+// (1.2 GB of weights read in turn).
 int launch_gemv_mx4(const qx_desc* d, const void* packed, const uint16_t* x, uint16_t* y, hipStream_t s) {
   return launch_gemv_rows<1>(d, packed, x, y, s);
 }
 
-// Two rows without tiles where a row of weights is long. us, and in the tiles: 22016x1024 6.4, 5.1; 4096x2048
-// 3.9, 3.9; 22016x4096 12.2, 12.1; 4096x4096 4.2, 4.9; 509x8192 4.2, 6.5; 8192x8192 10.4, 14.0; 16384x11008
-// 25.6, 25.9; three rows: 4096x4096 5.5, 5.0; 8192x8192 18.6, 14.0.
+// Two rows without tiles where a row of weights is long. us, and in the tiles: 22016x1024 6.2, 5.3; 4096x2048
+// 3.9, 4.5; 22016x4096 12.0, 12.2; 4096x4096 4.2, 5.9; 509x8192 4.2, 8.4; 8192x8192 10.4, 15.0; 16384x11008
+// 25.2, 25.8. Three rows, when that was chosen: 4096x4096 5.5, 5.0; 8192x8192 18.6, 14.0.
 int launch_gemm_mx4(const qx_desc* d, const void* packed, int m, const uint16_t* X, uint16_t* Y, hipStream_t s) {
   if (m == 1) return launch_gemv_rows<1>(d, packed, X, Y, s);
   if (m == 2 && d->k >= 2048) return launch_gemv_rows<2>(d, packed, X, Y, s);

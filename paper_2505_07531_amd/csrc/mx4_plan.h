@@ -13,12 +13,14 @@ namespace mx4 {
 // Cost in us at k = 128 K of up to 256 blocks, one a compute unit: us[0] + us[1] K; of every 256 more:
 // us[2] + us[3] K. One block of a shape with `one` set fills a compute unit, or nearly: those come in
 // whole rounds. Fitted to the times of 384 products (168 of one matrix, n = 256 to 22016, k = 512 to 11264,
-// m = 2 to 4096, and 216 of 4 to 128 experts, weights read from memory); where a shape is within 30 % of
-// the best, 96 of 100 are within 22 % (fp16 rows) and 27 % (MX4 rows). The shapes that they choose take 0.9
-// and 1.2 % more than the best of the measured ones in the mean, 2.9 and 2.0 % grouped by expert, where the
-// rows of an expert are a guess.
-// The last shape has several blocks a compute unit, for experts with few rows (32 experts of 2816x4096, 32
-// fp16 rows: 19.9 us, 24.7 in the best of the others; 64 of 2816x2048, 48 MX4 rows: 16.6, 18.4).
+// m = 2 to 4096, and 216 of 4 to 128 experts) before the reads of a unit were held together ahead of its
+// products. With the present kernels, on the same products (but those of two fp16 rows that take no tiles)
+// with 1.2 GB of weights read in turn, the shapes that the costs choose take 0.6 % (fp16 rows) and 1.6 % (MX4
+// rows) more than the best of all shapes in the mean, 3.6 and 2.3 % grouped by expert, where the rows of an
+// expert are a guess; at most 20 and 21 %, grouped 40 and 32 %. Where a shape is within 30 % of the best, 96
+// of 100 costs are within 21 to 31 % of its time.
+// The last shape has several blocks a compute unit, for experts with few rows (in the same run, 32 experts of
+// 2816x4096, 32 fp16 rows: 25.2 us, 31.4 in the best of the others; 64 of 2816x2048, 48 MX4 rows: 20.5, 21.7).
 struct ShapeCost {
   int mt, nt, wm, wn, wk, ks;
   bool one;
@@ -51,9 +53,9 @@ inline constexpr ShapeCost shapes<true>[kShapes] = {
     {8, 4, 2, 4, 1, 2, true, {6.73f, 0.981f, 5.95f, 1.15f}},
     {1, 2, 1, 1, 4, 1, true, {2.66f, 0.0883f, 0.285f, 0.0631f}},
 };
-// fp16 rows of one matrix do without the last shape: it is the best for 6 of the 168 products, by 4 to 19 %,
-// but a cost is too coarse to tell them from those where its blocks come out uneven over the compute units
-// (19088x7168, m = 2: 25.7 us, 19.1 in 16 x 32).
+// fp16 rows of one matrix do without the last shape: it is the best for 4 of the 165 products, by 3 to 11 %,
+// but a cost is too coarse to tell them from those where its blocks come out uneven over the compute units: it
+// would be chosen for 4, of which 3 then take 8 to 15 % more (13242x512, m = 3: 4.3 us, 3.8 in 16 x 32).
 template <bool A4>
 constexpr bool built(int shape, bool grouped) { return A4 || grouped || shape < kShapes - 1; }
 
@@ -69,7 +71,7 @@ inline float shape_us(const ShapeCost& s, float tiles, int n, int k, bool ragged
 // Row tiles of bm rows that m rows of `experts` experts take. Only the device knows their sizes: the rows
 // are taken as shared by as many experts as there can be, with shares that differ by a factor of two or
 // so. Then an expert has half a tile more than its rows fill, and few have less than one (32 experts of
-// 4096x1408, 4001 MX4 rows: 36 us in tiles of 128 x 128, 51 in 256 x 256, which counted as one tile
+// 4096x1408, 4001 MX4 rows: 42 us in tiles of 128 x 128, 51 in 256 x 256, which would count as one tile
 // an expert).
 inline float expert_tiles(int m, int experts, int bm) {
   const float used = (float)(experts < m ? experts : m), full = (float)m / (used * (float)bm);

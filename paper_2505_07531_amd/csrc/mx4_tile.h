@@ -19,14 +19,17 @@
 // order of the waves. The outputs of large tiles pass through LDS, so that stores write whole rows of
 // the tile (32-byte pieces: 9 us more of 183). The order of the sums is fixed: the same bits every time.
 //
-// Measured (us, and TFLOP/s): MX4 rows 22016x4096, m = 4096: 228 (3240); fp16
-// rows 11008x4096, m = 2001: 170 (1060), where a library product of fp16 matrices of 8192^3 reaches 1140; 32
-// experts of 2816x4096, 32 fp16 rows: 20.8 (5.0 TB/s). The largest tiles' time is a third products, the
-// rest the start and end of a tile (all compute units store at once) and loads. Deeper rings of smaller
-// stages there, and halves of a block's waves multiplying and loading in turn, were not faster (285 to 320 us
-// on the MX4 product at 265 then). Three buffers of small tiles gain a tenth where blocks are few and k is
-// long (4096x11008, 64 fp16 rows: 20.2 to 18.1 us) and lose far more where several share a compute unit
-// (22016x4096, 8 rows: 13.2 to 20.7): two buffers.
+// Measured (kernel trace, card warm; us, and TFLOP/s): MX4 rows 22016x4096, m = 4096: 242 (3050); fp16
+// rows 11008x4096, m = 2001: 180 (1000), where a library product of fp16 matrices of 8192^3 reaches 1140; 32
+// experts of 2816x4096, 32 fp16 rows: 20.9 (5.0 TB/s). The matrix cores are busy two fifths of the largest
+// tiles' time, the rest is the start and end of a tile (all compute units store at once) and loads.
+//
+// The pairs of times here and below are those of the step that chose between them, both sides in turn on one
+// card; later steps moved both. Deeper rings of smaller stages in the largest tiles, and halves of a block's
+// waves multiplying and loading in turn, were not faster (285 to 320 us on the MX4 product above, 265
+// without). Three buffers of small tiles gain a tenth where blocks are few and k is long (4096x11008, 64 fp16
+// rows: 20.2 to 18.1 us) and lose far more where several share a compute unit (22016x4096, 8 rows: 13.2 to
+// 20.7): two buffers.
 #pragma once
 
 #include <type_traits>
