@@ -204,11 +204,6 @@ def _chk(t, name: str, dtype, numel: int):
         raise ValueError(f"{name}: {t.numel()} elements, at least {numel} needed")
 
 
-def _ptrs(*tensors):
-    """Device pointers, taken only once every argument has been checked."""
-    return [None if t is None else t.data_ptr() for t in tensors]
-
-
 # The size follows from the six numbers alone, and asking the library for it took a good
 # part of a small call (a 4096x4096 codebook-3 GEMV from Python 10.8 us with it, two stream
 # objects' worth of torch.cuda.current_stream() and pointer objects; 7.2 us without).
@@ -255,14 +250,14 @@ def _here(stream, *tensors):
     return stream.cuda_stream
 
 
-def _new(stream, shape, dtype, device):
-    """A new tensor for a call to write; for one on a given stream from that stream's own memory,
-    since what the current stream freed it may still be writing."""
-    import torch
+def _new(stream, like, shape, dtype):
+    """A new tensor for a call to write, on the device of `like`; for one on a given stream from that
+    stream's own memory, since what the current stream freed it may still be writing."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+    import torch
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def qx_dequant(d: QxDesc, packed, out_kind: int, out, stream=None) -> None:
@@ -270,7 +265,7 @@ def qx_dequant(d: QxDesc, packed, out_kind: int, out, stream=None) -> None:
     _chk_packed(d, packed)
     _chk(out, "out", torch.float16 if out_kind == QX_OUT_F16 else torch.uint8, d.n * d.k)
     s = _here(stream, packed, out)
-    _check(load().qx_dequant(ctypes.byref(d), *_ptrs(packed), out_kind, *_ptrs(out), s), "qx_dequant")
+    _check(load().qx_dequant(ctypes.byref(d), packed.data_ptr(), out_kind, out.data_ptr(), s), "qx_dequant")
 
 
 def qx_gemv(d: QxDesc, packed, x, y, stream=None) -> None:
@@ -279,7 +274,7 @@ def qx_gemv(d: QxDesc, packed, x, y, stream=None) -> None:
     _chk(x, "x", torch.float16, d.k)
     _chk(y, "y", torch.float16, d.n)
     s = _here(stream, packed, x, y)
-    _check(load().qx_gemv(ctypes.byref(d), *_ptrs(packed, x, y), s), "qx_gemv")
+    _check(load().qx_gemv(ctypes.byref(d), packed.data_ptr(), x.data_ptr(), y.data_ptr(), s), "qx_gemv")
 
 
 def qx_gemv_a8(d: QxDesc, packed, x, y, stream=None) -> None:
@@ -288,7 +283,7 @@ def qx_gemv_a8(d: QxDesc, packed, x, y, stream=None) -> None:
     _chk(x, "x", torch.float16, d.k)
     _chk(y, "y", torch.float16, d.n)
     s = _here(stream, packed, x, y)
-    _check(load().qx_gemv_a8(ctypes.byref(d), *_ptrs(packed, x, y), s), "qx_gemv_a8")
+    _check(load().qx_gemv_a8(ctypes.byref(d), packed.data_ptr(), x.data_ptr(), y.data_ptr(), s), "qx_gemv_a8")
 
 
 def qx_gemm(d: QxDesc, packed, m: int, X, Y, stream=None) -> None:
@@ -299,8 +294,7 @@ def qx_gemm(d: QxDesc, packed, m: int, X, Y, stream=None) -> None:
     _chk(X, "X", torch.float16, m * d.k)
     _chk(Y, "Y", torch.float16, m * d.n)
     s = _here(stream, packed, X, Y)
-    p, x, y = _ptrs(packed, X, Y)
-    _check(load().qx_gemm(ctypes.byref(d), p, m, x, y, s), "qx_gemm")
+    _check(load().qx_gemm(ctypes.byref(d), packed.data_ptr(), m, X.data_ptr(), Y.data_ptr(), s), "qx_gemm")
 
 
 def qx_quantize_a8(m: int, k: int, X, Xq, sx, stream=None) -> None:
@@ -310,7 +304,7 @@ def qx_quantize_a8(m: int, k: int, X, Xq, sx, stream=None) -> None:
     _chk(Xq, "Xq", torch.int8, m * k)
     _chk(sx, "sx", torch.float32, m)
     s = _here(stream, X, Xq, sx)
-    _check(load().qx_quantize_a8(m, k, *_ptrs(X, Xq, sx), s), "qx_quantize_a8")
+    _check(load().qx_quantize_a8(m, k, X.data_ptr(), Xq.data_ptr(), sx.data_ptr(), s), "qx_quantize_a8")
 
 
 def qx_gemm_a8(d: QxDesc, packed, m: int, Xq, sx, Y, stream=None) -> None:
@@ -322,8 +316,8 @@ def qx_gemm_a8(d: QxDesc, packed, m: int, Xq, sx, Y, stream=None) -> None:
     _chk(sx, "sx", torch.float32, m)
     _chk(Y, "Y", torch.float16, m * d.n)
     s = _here(stream, packed, Xq, sx, Y)
-    p, xq, s_, y = _ptrs(packed, Xq, sx, Y)
-    _check(load().qx_gemm_a8(ctypes.byref(d), p, m, xq, s_, y, s), "qx_gemm_a8")
+    _check(load().qx_gemm_a8(ctypes.byref(d), packed.data_ptr(), m, Xq.data_ptr(), sx.data_ptr(), Y.data_ptr(), s),
+           "qx_gemm_a8")
 
 
 def qx_quantize_mx4(m: int, k: int, X, packed, stream=None) -> None:
@@ -333,7 +327,7 @@ def qx_quantize_mx4(m: int, k: int, X, packed, stream=None) -> None:
     _chk(X, "X", torch.float16, m * k)
     _chk(packed, "packed", torch.uint8, m * k // 32 * 17)
     s = _here(stream, X, packed)
-    _check(load().qx_quantize_mx4(m, k, *_ptrs(X, packed), s), "qx_quantize_mx4")
+    _check(load().qx_quantize_mx4(m, k, X.data_ptr(), packed.data_ptr(), s), "qx_quantize_mx4")
 
 
 def _mx4_rows(Xq, m: int, k: int):
@@ -348,8 +342,7 @@ def qx_gemm_a4(d: QxDesc, packed, m: int, Xq, Y, stream=None) -> None:
     _mx4_rows(Xq, m, d.k)
     _chk(Y, "Y", torch.float16, m * d.n)
     s = _here(stream, packed, Xq, Y)
-    p, x, y = _ptrs(packed, Xq, Y)
-    _check(load().qx_gemm_a4(ctypes.byref(d), p, m, x, y, s), "qx_gemm_a4")
+    _check(load().qx_gemm_a4(ctypes.byref(d), packed.data_ptr(), m, Xq.data_ptr(), Y.data_ptr(), s), "qx_gemm_a4")
 
 
 def _chk_experts(d: QxDesc, packed, offsets):
@@ -373,8 +366,8 @@ def qx_gemm_grouped(d: QxDesc, packed, m: int, X, offsets, Y, stream=None) -> No
     _chk(X, "X", torch.float16, m * d.k)
     _chk(Y, "Y", torch.float16, m * d.n)
     s = _here(stream, packed, X, offsets, Y)
-    p, x, o, y = _ptrs(packed, X, offsets, Y)
-    _check(load().qx_gemm_grouped(ctypes.byref(d), p, stride, experts, m, x, o, y, s), "qx_gemm_grouped")
+    _check(load().qx_gemm_grouped(ctypes.byref(d), packed.data_ptr(), stride, experts, m, X.data_ptr(),
+                                  offsets.data_ptr(), Y.data_ptr(), s), "qx_gemm_grouped")
 
 
 def qx_gemm_a4_grouped(d: QxDesc, packed, m: int, Xq, offsets, Y, stream=None) -> None:
@@ -384,15 +377,15 @@ def qx_gemm_a4_grouped(d: QxDesc, packed, m: int, Xq, offsets, Y, stream=None) -
     _mx4_rows(Xq, m, d.k)
     _chk(Y, "Y", torch.float16, m * d.n)
     s = _here(stream, packed, Xq, offsets, Y)
-    p, x, o, y = _ptrs(packed, Xq, offsets, Y)
-    _check(load().qx_gemm_a4_grouped(ctypes.byref(d), p, stride, experts, m, x, o, y, s), "qx_gemm_a4_grouped")
+    _check(load().qx_gemm_a4_grouped(ctypes.byref(d), packed.data_ptr(), stride, experts, m, Xq.data_ptr(),
+                                     offsets.data_ptr(), Y.data_ptr(), s), "qx_gemm_a4_grouped")
 
 
 def quantize_mx4(X, stream=None) -> "PackedWeight":
     """An fp16 device tensor [m][k], weights or activations, rounded to MX4 where it lies."""
     import torch
     m, k = X.shape
-    out = _new(stream, m * k // 32 * 17, torch.uint8, X.device)
+    out = _new(stream, X, m * k // 32 * 17, torch.uint8)
     qx_quantize_mx4(m, k, X, out, stream)
     return PackedWeight._around(QxDesc(m, k, 4, 32, QX_MX4, 0), out, m * k // 32 * 17)
 
@@ -401,8 +394,8 @@ def quantize_a8(X, stream=None):
     """(Xq int8 [m][k], sx fp32 [m]) of an fp16 [m][k] device tensor."""
     import torch
     m, k = X.shape
-    Xq = _new(stream, (m, k), torch.int8, X.device)
-    sx = _new(stream, m, torch.float32, X.device)
+    Xq = _new(stream, X, (m, k), torch.int8)
+    sx = _new(stream, X, m, torch.float32)
     qx_quantize_a8(m, k, X, Xq, sx, stream)
     return Xq, sx
 
@@ -443,14 +436,14 @@ class PackedWeight:
     def dequant(self, out_kind: int = QX_OUT_F16, stream=None):
         import torch
         dt = torch.float16 if out_kind == QX_OUT_F16 else torch.uint8
-        out = _new(stream, (self.desc.n, self.desc.k), dt, self.data.device)
+        out = _new(stream, self.data, (self.desc.n, self.desc.k), dt)
         qx_dequant(self.desc, self.data, out_kind, out, stream)
         return out
 
     def gemv(self, x, y=None, stream=None):
         import torch
         if y is None:
-            y = _new(stream, self.desc.n, torch.float16, x.device)
+            y = _new(stream, x, self.desc.n, torch.float16)
         qx_gemv(self.desc, self.data, x, y, stream)
         return y
 
@@ -458,14 +451,14 @@ class PackedWeight:
         import torch
         m = Xq.shape[0]
         if Y is None:
-            Y = _new(stream, (m, self.desc.n), torch.float16, Xq.device)
+            Y = _new(stream, Xq, (m, self.desc.n), torch.float16)
         qx_gemm_a8(self.desc, self.data, m, Xq, sx, Y, stream)
         return Y
 
     def gemv_a8(self, x, y=None, stream=None):
         import torch
         if y is None:
-            y = _new(stream, self.desc.n, torch.float16, x.device)
+            y = _new(stream, x, self.desc.n, torch.float16)
         qx_gemv_a8(self.desc, self.data, x, y, stream)
         return y
 
@@ -473,7 +466,7 @@ class PackedWeight:
         import torch
         m = X.shape[0]
         if Y is None:
-            Y = _new(stream, (m, self.desc.n), torch.float16, X.device)
+            Y = _new(stream, X, (m, self.desc.n), torch.float16)
         qx_gemm(self.desc, self.data, m, X, Y, stream)
         return Y
 
@@ -482,7 +475,7 @@ class PackedWeight:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            Y = _new(stream, (m, self.desc.n), torch.float16, Xq.data.device)
+            Y = _new(stream, Xq.data, (m, self.desc.n), torch.float16)
         qx_gemm_a4(self.desc, self.data, m, Xq.data, Y, stream)
         return Y
 
@@ -521,7 +514,7 @@ class PackedExperts:
         import torch
         m = X.shape[0]
         if Y is None:
-            Y = _new(stream, (m, self.desc.n), torch.float16, X.device)
+            Y = _new(stream, X, (m, self.desc.n), torch.float16)
         qx_gemm_grouped(self.desc, self.data, m, X, offsets, Y, stream)
         return Y
 
@@ -530,6 +523,6 @@ class PackedExperts:
         import torch
         m = _rows_of(Xq, self.desc.k)
         if Y is None:
-            Y = _new(stream, (m, self.desc.n), torch.float16, Xq.data.device)
+            Y = _new(stream, Xq.data, (m, self.desc.n), torch.float16)
         qx_gemm_a4_grouped(self.desc, self.data, m, Xq.data, offsets, Y, stream)
         return Y

@@ -17,6 +17,7 @@ N, K, M = 64, 256, 4
 class Tensor:
     """Stand-in for a device tensor of device 1; nothing reaches the library."""
     is_cuda, device = True, "cuda:1"
+    made = None  # the Allocations of a test
 
     def __init__(self, dtype, *shape):
         self.dtype, self.shape = dtype, shape
@@ -32,6 +33,9 @@ class Tensor:
 
     def get_device(self):
         return 1
+
+    def new_empty(self, shape, dtype=None):
+        return self.made.empty(shape, dtype)
 
     def data_ptr(self):
         raise AssertionError("a pointer was taken: the call would have launched")
@@ -75,6 +79,7 @@ class Allocations:
     def __init__(self, monkeypatch, current):
         self.now, self.on = None, []
         monkeypatch.setattr(torch, "empty", self.empty)
+        monkeypatch.setattr(Tensor, "made", self)
         monkeypatch.setattr(torch.cuda, "stream", self.stream)
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current, raising=False)
         monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 5, raising=False)
